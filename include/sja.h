@@ -365,6 +365,97 @@ sja_status sja_advertise_power_caps(sja_ctx* ctx, const uint32_t* cap_W, sja_mem
 sja_status sja_update_profile(sja_ctx* ctx, uint32_t job, uint32_t n_steps, const uint32_t* dur_ms,
                               const uint32_t* mem_MiB, sja_memspace where);
 
+/*
+ * Forecasting side.  The profiles the round works on are forecasts: "predictive guidance" of Section 3.8, refined as
+ * predictions improve (Section 3.9), by models the paper leaves to further work (Section 5.3).  The calls below are
+ * the operators of a sequence model that makes them, over the histories of many jobs at once: the recurrent scan of a
+ * layer (sja_ssm_prompt over the histories, sja_ssm_step when jobs have advanced by a step) and the statistics of
+ * the model's answers (sja_token_stats: how likely the observed values were, how sure the model is, and which values
+ * it expects -- the envelope U(t) = Q_{1-eps}[M(t)] is taken from those).  Matrix products between them are the
+ * caller's.  They need no loaded profiles, use none of the round's state, work on the context's stream with device
+ * pointers only, and never wait for the GPU (a call that needs a larger workspace than any before it does).
+ */
+typedef enum { SJA_F32 = 0, SJA_F16 = 1, SJA_BF16 = 2 } sja_dtype;
+
+/*
+ * One layer's selective state space scan with its short causal convolution.  Per job, token t, channel d in group
+ * g = d / (D / G) and state n:
+ *
+ *     row_t = [x (D) | B (G x N) | C (G x N)]        u_t = silu(conv_b + sum_{w < W} conv_w[:, w] row_{t-W+1+w})
+ *     dt_t  = softplus(dt_t + dt_bias)                (x, B, C below are the parts of u_t)
+ *     h_t[d, n] = exp(dt_t[d] A[d, n]) h_{t-1}[d, n] + dt_t[d] x_t[d] B_t[g, n]
+ *     y_t[d]    = (sum_n C_t[g, n] h_t[d, n] + skip[d] x_t[d]) silu(z_t[d])
+ *
+ * All sums and states are 32-bit; y is rounded once.  W = 0 leaves row_t as it is (no convolution, no silu).
+ * Rows may lie apart (strides in elements, a row itself is contiguous); no alignment beyond the element's own.
+ * y must not overlap an input.  Infinities and NaN travel as the formulas carry them, within their own job only.
+ *
+ * Between calls a job lives in a slot of two pools: its states, and the W - 1 rows before its next token (oldest
+ * first, zero before a job's first row).  slots[s] is job s's slot (NULL: slot s); a job whose slot is outside
+ * 0 .. n_slots - 1 starts from zero and is not kept.  Two jobs of one call must not share a slot.
+ */
+typedef struct {
+    uint32_t dtype;              /* sja_dtype of xbc, dt, z, y and history */
+    uint32_t n_channels;         /* D, 1 .. 2^20 */
+    uint32_t n_state;            /* N, 1 .. 128 */
+    uint32_t n_groups;           /* G, divides D; G * N <= 4096 */
+    uint32_t conv_width;         /* W, 0 .. 4 */
+    uint32_t n_slots;            /* size of the pools */
+    const float* A;              /* [D, N] */
+    const float* skip;           /* [D] or NULL (0) */
+    const float* dt_bias;        /* [D] or NULL (0) */
+    const float* conv_w;         /* [D + 2GN, W]; NULL iff W = 0 */
+    const float* conv_b;         /* [D + 2GN] or NULL (0) */
+    const void* xbc;             /* rows of D + 2GN */
+    const void* dt;              /* rows of D */
+    const void* z;               /* rows of D, or NULL (no gate) */
+    void* y;                     /* rows of D */
+    int64_t xbc_stride, dt_stride, z_stride, y_stride;
+    float* state;                /* [n_slots, D, N]; sja_ssm_prompt: NULL = not kept */
+    void* history;               /* [n_slots, W - 1, D + 2GN]; NULL = zero and not kept */
+    const int32_t* slots;        /* [S] or NULL */
+} sja_ssm;
+
+/*
+ * The scan over S jobs' tokens, T in all, packed one job after another: job s owns rows off[s] .. off[s + 1] - 1
+ * (off u64[S + 1] in device memory, off[0] = 0, ascending, off[S] = T; a job may be empty).  resume = 1: every job
+ * goes on from its slot; 0: every job starts from zero.  Either way its slot holds the state and the last rows
+ * afterwards (an empty job's: unchanged, or zero).  Offsets are not read by the host: rows that they do not cover
+ * are left unwritten, and none outside 0 .. T - 1 is touched.
+ */
+sja_status sja_ssm_prompt(sja_ctx* ctx, const sja_ssm* ssm, uint32_t S, uint64_t T, const uint64_t* off,
+                          uint32_t resume);
+
+/* One token for each of S jobs, row s for job s, continued from and kept in its slot (`state` is needed). */
+sja_status sja_ssm_step(sja_ctx* ctx, const sja_ssm* ssm, uint32_t S);
+
+/*
+ * Statistics of R rows of V logits, l = scale * logits (scale > 0), lse = log sum exp(l):
+ *   logp[r]      l[token] - lse; 0 for a negative token (a position that is not scored), NaN for one >= V
+ *   entropy[r]   lse - sum p l, p = exp(l - lse), in nats; an entry of -inf (masked) adds nothing
+ *   top_ids      the `top` largest logits, in descending order, ties to the lowest index (-0 = 0; NaN sorts below
+ *                -inf); entries beyond V are -1
+ *   top_logp     their l - lse; -inf beyond V
+ * A row of nothing but -inf has entropy 0, and -inf for every log probability; a NaN or +inf in a row makes its
+ * log probabilities and entropy NaN (an entry of -inf stays -inf).  Sums are 32-bit.  top is 0 .. 32; every output
+ * may be NULL.  `tokens` (needed for logp) are int64.  row_stride is in elements.
+ */
+typedef struct {
+    uint32_t dtype;              /* sja_dtype of logits */
+    uint32_t top;
+    uint64_t n_rows;
+    uint32_t vocab;              /* V, 1 .. 2^30 */
+    float scale;
+    const void* logits;
+    int64_t row_stride;
+    const int64_t* tokens;       /* [R] or NULL */
+    float* logp;                 /* [R] */
+    float* entropy;              /* [R] */
+    float* top_logp;             /* [R, top] */
+    int32_t* top_ids;            /* [R, top] */
+} sja_token_rows;
+sja_status sja_token_stats(sja_ctx* ctx, const sja_token_rows* rows);
+
 /* Copy the G awards of the last select (with `granted` set if it was committed). */
 sja_status sja_get_awards(sja_ctx* ctx, sja_award* out, sja_memspace where);
 

@@ -1,7 +1,8 @@
 """ctypes binding of libsja.so.  Argument marshalling only: every step runs in the library.
 
 Arrays may be numpy arrays (host memory) or torch CUDA tensors (device memory); the
-memory space is inferred per call and all arrays of one call must agree.
+memory space is inferred per call and all arrays of one call must agree.  The forecasting
+side (:class:`SsmLayer`, :meth:`Sja.token_stats`) takes torch CUDA tensors only.
 """
 from __future__ import annotations
 
@@ -35,6 +36,7 @@ EXPORTS = [
     "sja_create", "sja_destroy", "sja_load_profiles", "sja_advertise", "sja_select", "sja_select_static", "sja_commit", "sja_commit_masked", "sja_round_reauction", "sja_set_duration_bounds", "sja_set_window_options", "sja_set_hysteresis", "sja_set_locality", "sja_get_locality", "sja_update_profile", "sja_load_power", "sja_advertise_power_caps", "sja_get_bids", "sja_reduce_bids",
     "sja_get_awards", "sja_get_state", "sja_scan_size", "sja_get_scan", "sja_profile_enable",
     "sja_profile_read", "sja_last_error", "sja_debug_fail_alloc",
+    "sja_ssm_prompt", "sja_ssm_step", "sja_token_stats",
 ]
 
 
@@ -49,6 +51,22 @@ class SjaTiming(ctypes.Structure):
                 ("scan_launches", ctypes.c_uint32), ("prep_launches", ctypes.c_uint32),
                 ("advertise_launches", ctypes.c_uint32), ("select_launches", ctypes.c_uint32),
                 ("commit_launches", ctypes.c_uint32)]
+
+
+_p, _u32, _i64 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_int64
+
+
+class SjaSsm(ctypes.Structure):
+    _fields_ = [("dtype", _u32), ("n_channels", _u32), ("n_state", _u32), ("n_groups", _u32), ("conv_width", _u32),
+                ("n_slots", _u32), ("A", _p), ("skip", _p), ("dt_bias", _p), ("conv_w", _p), ("conv_b", _p),
+                ("xbc", _p), ("dt", _p), ("z", _p), ("y", _p), ("xbc_stride", _i64), ("dt_stride", _i64),
+                ("z_stride", _i64), ("y_stride", _i64), ("state", _p), ("history", _p), ("slots", _p)]
+
+
+class SjaTokenRows(ctypes.Structure):
+    _fields_ = [("dtype", _u32), ("top", _u32), ("n_rows", ctypes.c_uint64), ("vocab", _u32), ("scale", ctypes.c_float),
+                ("logits", _p), ("row_stride", _i64), ("tokens", _p), ("logp", _p), ("entropy", _p), ("top_logp", _p),
+                ("top_ids", _p)]
 
 
 class SjaError(RuntimeError):
@@ -98,6 +116,9 @@ def load_library() -> ctypes.CDLL:
     lib.sja_profile_read.argtypes = [vp, ctypes.POINTER(SjaTiming)]
     lib.sja_last_error.argtypes = [vp]
     lib.sja_debug_fail_alloc.argtypes = [vp, i32]
+    lib.sja_ssm_prompt.argtypes = [vp, ctypes.POINTER(SjaSsm), u32, ctypes.c_uint64, vp, u32]
+    lib.sja_ssm_step.argtypes = [vp, ctypes.POINTER(SjaSsm), u32]
+    lib.sja_token_stats.argtypes = [vp, ctypes.POINTER(SjaTokenRows)]
     lib.sja_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name != "sja_last_error":
@@ -130,6 +151,14 @@ def _ptr_space(a, space: Optional[int], np_dtype=None):
     return ptr, sp, keep
 
 
+_DTYPE_CODES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+
+
+def _torch():
+    import torch
+    return torch
+
+
 class Sja:
     """One scheduler context on one CUDA device (wraps ``sja_ctx``)."""
 
@@ -140,6 +169,7 @@ class Sja:
         if st != SJA_OK:
             self._h = ctypes.c_void_p()
             raise SjaError(st, "sja_create failed (is a CUDA device present?)")
+        self.device, self.stream = int(device), int(stream or 0)
         self.n_jobs = 0
         self.n_gaps = 0
 
@@ -369,6 +399,75 @@ class Sja:
                                            M.ctypes.data, S.ctypes.data, W.ctypes.data, MEM_HOST))
         return dict(boff=boff, k=k, D=D, M=M, S=S, W=W)
 
+    # -- sja_ssm_prompt / sja_ssm_step
+    def ssm_layer(self, A, conv_w=None, conv_b=None, skip=None, dt_bias=None, n_groups: int = 1) -> "SsmLayer":
+        """The weights of one layer's scan, checked once: see :class:`SsmLayer`."""
+        return SsmLayer(self, A, conv_w, conv_b, skip, dt_bias, n_groups)
+
+    # -- sja_token_stats
+    def token_stats(self, logits, tokens=None, top: int = 0, scale: float = 1.0) -> dict:
+        """Statistics of the rows of ``logits`` (R, V), scaled by ``scale`` (one over a temperature): a dict of
+        ``entropy`` f32 (R,) in nats; with ``tokens`` (int64 (R,); negative = not scored, 0) their log
+        probabilities ``logp`` f32 (R,); with ``top`` (up to 32) the most likely tokens ``top_ids`` i32 (R, top) in
+        descending order, ties to the lowest, and their ``top_logp`` f32 (R, top)."""
+        code = self._rows("logits", logits, None, None)
+        R, V = logits.shape
+        if tokens is not None:
+            self._flat("tokens", tokens, "int64", (R,))
+        a = SjaTokenRows(dtype=code, top=int(top), n_rows=R, vocab=V, scale=float(scale), logits=logits.data_ptr(),
+                         row_stride=max(logits.stride(0), V) if R < 2 else logits.stride(0))
+        torch, used = _torch(), (logits, tokens)
+        out = {"entropy": self._empty((R,), torch.float32, logits, used)}
+        a.entropy = out["entropy"].data_ptr()
+        if tokens is not None:
+            out["logp"] = self._empty((R,), torch.float32, logits, ())
+            a.tokens, a.logp = tokens.data_ptr(), out["logp"].data_ptr()
+        if 0 < top <= 32:
+            out["top_logp"] = self._empty((R, int(top)), torch.float32, logits, ())
+            out["top_ids"] = self._empty((R, int(top)), torch.int32, logits, ())
+            a.top_logp, a.top_ids = out["top_logp"].data_ptr(), out["top_ids"].data_ptr()
+        elif top == 0:
+            out["top_logp"] = self._empty((R, 0), torch.float32, logits, ())
+            out["top_ids"] = self._empty((R, 0), torch.int32, logits, ())
+        self._check(self._lib.sja_token_stats(self._h, ctypes.byref(a)))
+        return out
+
+    def _rows(self, name, t, shape, dtype) -> int:
+        """A CUDA tensor of rows (each contiguous) on this context's device; returns its sja_dtype."""
+        code = _DTYPE_CODES.get(str(getattr(t, "dtype", "")))
+        if code is None or not t.is_cuda or t.device.index != self.device:
+            raise TypeError(f"{name}: a float32, float16 or bfloat16 tensor on CUDA device {self.device} is needed")
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError(f"{name}: {t.dtype}, where the rows are {dtype}")
+        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}" + (f", not {shape}" if shape else " is not (rows, columns)"))
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        return code
+
+    def _flat(self, name, t, dtype, shape) -> None:
+        """A contiguous CUDA tensor of one type and shape (None in the shape: any length)."""
+        if not _is_torch(t) or str(t.dtype) != "torch." + dtype or not t.is_cuda or t.device.index != self.device:
+            raise TypeError(f"{name}: a {dtype} tensor on CUDA device {self.device} is needed")
+        if t.dim() != len(shape) or any(w is not None and v != w for v, w in zip(t.shape, shape)):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
+
+    def _empty(self, shape, dtype, like, used):
+        """A new tensor for a result of this call.  Where torch works on another stream than the context, the memory
+        belongs to the context's stream, and the tensors the call uses are kept until that stream is through."""
+        torch = _torch()
+        if torch.cuda.current_stream(self.device).cuda_stream == self.stream:
+            return torch.empty(shape, dtype=dtype, device=like.device)
+        mine = torch.cuda.ExternalStream(self.stream, device=self.device)
+        for t in used:
+            if t is not None:
+                t.record_stream(mine)
+        with torch.cuda.stream(mine):
+            out = torch.empty(shape, dtype=dtype, device=like.device)
+        return out
+
     # -- sja_debug_fail_alloc
     def debug_fail_alloc(self, nth: int) -> None:
         """Host-side fault injection: the nth growing allocation from now reports SJA_ERR_OOM (0 = off)."""
@@ -383,3 +482,90 @@ class Sja:
         t = SjaTiming()
         self._check(self._lib.sja_profile_read(self._h, ctypes.byref(t)))
         return {name: getattr(t, name) for name, _ in SjaTiming._fields_}
+
+
+class SsmLayer:
+    """One layer's selective state space scan with its short convolution (``sja_ssm`` in include/sja.h).
+
+    Weights are float32: ``A`` (D, N); ``skip`` and ``dt_bias`` (D,); ``conv_w`` (D + 2GN, W) and ``conv_b``
+    (D + 2GN,).  They are used where they lie and must stay alive and in place.  Rows of ``xbc`` (T, D + 2GN),
+    ``dt`` and ``z`` (T, D) are float32, float16 or bfloat16 and may be slices of a wider tensor.  ``state``
+    (n_slots, D, N) float32 and ``history`` (n_slots, W - 1, D + 2GN) in the rows' type are updated in place;
+    ``slots`` int32 (S,) says which belong to which job (None: slot s).  Work is queued on the context's stream.
+    """
+
+    def __init__(self, ctx: Sja, A, conv_w=None, conv_b=None, skip=None, dt_bias=None, n_groups: int = 1):
+        ctx._flat("A", A, "float32", (None, None))
+        D, N = A.shape
+        G = int(n_groups)
+        if G < 1 or D % G:
+            raise ValueError(f"n_groups {G} must divide the {D} channels")
+        rows = D + 2 * G * N
+        for name, t, shape in (("skip", skip, (D,)), ("dt_bias", dt_bias, (D,)), ("conv_w", conv_w, (rows, None)),
+                               ("conv_b", conv_b, (rows,))):
+            if t is not None:
+                ctx._flat(name, t, "float32", shape)
+        self.ctx, self.D, self.N, self.G, self.rows = ctx, D, N, G, rows
+        self.W = 0 if conv_w is None else int(conv_w.shape[1])
+        self._keep = (A, conv_w, conv_b, skip, dt_bias)
+        ptr = [None if t is None else t.data_ptr() for t in self._keep]
+        self._args = SjaSsm(n_channels=D, n_state=N, n_groups=G, conv_width=self.W, A=ptr[0], conv_w=ptr[1], conv_b=ptr[2],
+                            skip=ptr[3], dt_bias=ptr[4])
+
+    def _fill(self, xbc, dt, z, state, history, slots, n_jobs, out, more=()):
+        """Check one call's tensors and write them into the call's arguments; returns (arguments, y)."""
+        ctx = self.ctx
+        code = ctx._rows("xbc", xbc, None, None)
+        T = xbc.shape[0]
+        if xbc.shape[1] != self.rows:
+            raise ValueError(f"xbc: rows of {xbc.shape[1]}, not D + 2GN = {self.rows}")
+        ctx._rows("dt", dt, (T, self.D), xbc.dtype)
+        if z is not None:
+            ctx._rows("z", z, (T, self.D), xbc.dtype)
+        n_slots = n_jobs
+        if state is not None:
+            ctx._flat("state", state, "float32", (None, self.D, self.N))
+            n_slots = state.shape[0]
+        if history is not None:
+            ctx._flat("history", history, str(xbc.dtype)[6:], (None if state is None else n_slots, max(self.W - 1, 0), self.rows))
+            n_slots = history.shape[0]
+        if slots is not None:
+            ctx._flat("slots", slots, "int32", (n_jobs,))
+        if out is None:
+            out = ctx._empty((T, self.D), xbc.dtype, xbc, (xbc, dt, z, state, history, slots) + tuple(more))
+        else:
+            ctx._rows("out", out, (T, self.D), xbc.dtype)
+        a = SjaSsm.from_buffer_copy(self._args)
+        a.dtype, a.n_slots = code, n_slots
+        a.xbc, a.dt, a.y = xbc.data_ptr(), dt.data_ptr(), out.data_ptr()
+        a.xbc_stride, a.dt_stride, a.y_stride = xbc.stride(0), dt.stride(0), out.stride(0)
+        if z is not None:
+            a.z, a.z_stride = z.data_ptr(), z.stride(0)
+        if T < 2:                                       # the stride of a single row says nothing
+            a.xbc_stride, a.dt_stride, a.z_stride, a.y_stride = self.rows, self.D, self.D, self.D
+        if state is not None:
+            a.state = state.data_ptr()
+        if history is not None and self.W > 1:
+            a.history = history.data_ptr()
+        if slots is not None:
+            a.slots = slots.data_ptr()
+        return a, out
+
+    def prompt(self, xbc, dt, off, state=None, history=None, z=None, slots=None, resume: bool = False, out=None):
+        """sja_ssm_prompt: the packed tokens of S jobs, job s at rows ``off[s]`` .. ``off[s + 1] - 1`` (``off`` int64
+        (S + 1,) on the device).  ``resume``: go on from the slots instead of from zero.  Returns y (T, D)."""
+        ctx = self.ctx
+        ctx._flat("off", off, "int64", (None,))
+        S = off.shape[0] - 1
+        if S < 0:
+            raise ValueError("off: needs one entry per job and one more")
+        a, y = self._fill(xbc, dt, z, state, history, slots, S, out, (off,))
+        ctx._check(ctx._lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), S, xbc.shape[0], off.data_ptr(), 1 if resume else 0))
+        return y
+
+    def step(self, xbc, dt, state, history=None, z=None, slots=None, out=None):
+        """sja_ssm_step: one token for each of S jobs, continued from and kept in their slots.  Returns y (S, D)."""
+        ctx = self.ctx
+        a, y = self._fill(xbc, dt, z, state, history, slots, xbc.shape[0], out)
+        ctx._check(ctx._lib.sja_ssm_step(ctx._h, ctypes.byref(a), xbc.shape[0]))
+        return y

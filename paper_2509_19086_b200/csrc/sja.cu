@@ -20,6 +20,8 @@
 #include "sja_update.cuh"
 #include "sja_power.cuh"
 #include "sja_shard.cuh"
+#include "sja_ssm.cuh"
+#include "sja_tokens.cuh"
 
 using namespace sja;
 
@@ -87,6 +89,7 @@ struct sja_ctx {
     DevBuf gaps, sgaps, gap_info, gap_rank, awards, widx, partial, winners;
     DevBuf sgaps_alt, blocked, n_active, accept;   // re-auction: second ordered gap list, per-job block flags, gap counter
     DevBuf dirty;                                  // re-auction: job chunks whose candidate rows have to be found again
+    DevBuf ssm_ws;                                 // sja_ssm_prompt: what the segments of the token axis hand on
 
     // profiling
     int prof = 0;                      // 0 off, 1 every phase, 2 the scan kernel only
@@ -619,7 +622,7 @@ sja_status sja_destroy(sja_ctx* c) {
     DevBuf* bufs[] = {&c->st_off, &c->st_d, &c->st_m, &c->st_s, &c->st_p, &c->st_ready, &c->st_wait, &c->st_prio, &c->p, &c->ready, &c->pb, &c->Dp,
                       &c->Wp, &c->wait, &c->prio, &c->nbj, &c->cta_tot, &c->cta_base, &c->boff, &c->boff_next, &c->A, &c->B, &c->jobwin,
                       &c->flags, &c->counter, &c->n_granted, &c->long_list, &c->gaps, &c->sgaps, &c->gap_info, &c->gap_rank, &c->sgaps_alt, &c->dirty, &c->blocked, &c->n_active, &c->accept, &c->deadline, &c->ckpt, &c->last_slice, &c->PW, &c->caps, &c->st_power, &c->st_bids, &c->st_accept, &c->st_global, &c->upd_d, &c->upd_m, &c->upd_scratch, &c->upd_status, &c->awards, &c->widx, &c->partial,
-                      &c->winners};
+                      &c->winners, &c->ssm_ws};
     for (DevBuf* b : bufs) release(*b);
     for (ProfSpan& s : c->spans) { cudaEventDestroy(s.a); cudaEventDestroy(s.b); }
     for (cudaEvent_t e : c->free_events) cudaEventDestroy(e);
@@ -1445,6 +1448,196 @@ sja_status sja_get_scan(sja_ctx* c, uint64_t* boff, uint32_t* k, uint32_t* D, ui
     for (DevBuf& b : tmp) release(b);
     if (st == SJA_OK && e != cudaSuccess) return cuda_fail(c, e, "sja_get_scan");
     return st;
+}
+
+}  // extern "C"
+
+// =======================================================================================
+// Forecasting side: the recurrent scan of a sequence model, and the statistics of its answers.
+namespace {
+
+// Instance of the prompt kernel for N states: one thread holds two channels and up to 16 of their states, wider
+// states are shared by 2, 4 or 8 lanes.
+struct SsmShape { uint32_t K, lanes; uint32_t channels() const { return 32u / lanes * 2u; } };
+SsmShape ssm_shape(uint32_t N) {
+    if (N <= 8u) return {8u, 1u};
+    if (N <= 16u) return {16u, 1u};
+    if (N <= 32u) return {16u, 2u};
+    if (N <= 64u) return {16u, 4u};
+    return {16u, 8u};
+}
+
+template <typename T, bool CARRY>
+void launch_ssm_prompt(const SsmShape& sh, dim3 grid, uint32_t threads, cudaStream_t stream, const SsmArgs& a) {
+    if (sh.K == 8u) launch_dep(ssm_prompt_kernel<T, 8, 1, 2, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.lanes == 1u) launch_dep(ssm_prompt_kernel<T, 16, 1, 2, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.lanes == 2u) launch_dep(ssm_prompt_kernel<T, 16, 2, 2, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.lanes == 4u) launch_dep(ssm_prompt_kernel<T, 16, 4, 2, CARRY>, grid, threads, 0, stream, a);
+    else launch_dep(ssm_prompt_kernel<T, 16, 8, 2, CARRY>, grid, threads, 0, stream, a);
+}
+
+bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0; }
+size_t dtype_size(uint32_t dtype) { return dtype == SJA_F32 ? 4u : 2u; }
+
+// Argument checks shared by the two forms of the scan; fills the kernel arguments.
+sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, const char* who, SsmArgs& a) {
+    if (!m) return fail(c, SJA_ERR_INVALID_ARG, "%s: ssm is NULL", who);
+    if (m->dtype > SJA_BF16) return fail(c, SJA_ERR_INVALID_ARG, "%s: unknown dtype %u", who, m->dtype);
+    const uint64_t D = m->n_channels, N = m->n_state, G = m->n_groups;
+    if (D < 1 || D > (1u << 20)) return fail(c, SJA_ERR_INVALID_ARG, "%s: n_channels %u not in 1 .. 2^20", who, m->n_channels);
+    if (N < 1 || N > SSM_MAX_STATE) return fail(c, SJA_ERR_INVALID_ARG, "%s: n_state %u not in 1 .. 128", who, m->n_state);
+    if (G < 1 || D % G != 0 || G * N > 4096)
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: n_groups %u must divide n_channels, with n_groups * n_state <= 4096", who, m->n_groups);
+    if (m->conv_width > SSM_MAX_WIDTH) return fail(c, SJA_ERR_INVALID_ARG, "%s: conv_width %u not in 0 .. 4", who, m->conv_width);
+    if ((m->conv_width == 0) != (m->conv_w == nullptr))
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: conv_w goes with conv_width >= 1", who);
+    if (!m->A || (n_rows && (!m->xbc || !m->dt || !m->y))) return fail(c, SJA_ERR_INVALID_ARG, "%s: A, xbc, dt or y is NULL", who);
+    const int64_t rows = (int64_t)(D + 2 * G * N), d = (int64_t)D;
+    if (m->xbc_stride < rows || m->dt_stride < d || m->y_stride < d || (m->z && m->z_stride < d))
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: a row stride is shorter than its row", who);
+    const size_t e = dtype_size(m->dtype);
+    if (!aligned_to(m->xbc, e) || !aligned_to(m->dt, e) || !aligned_to(m->z, e) || !aligned_to(m->y, e) || !aligned_to(m->history, e) ||
+        !aligned_to(m->A, 4) || !aligned_to(m->skip, 4) || !aligned_to(m->dt_bias, 4) || !aligned_to(m->conv_w, 4) ||
+        !aligned_to(m->conv_b, 4) || !aligned_to(m->state, 4) || !aligned_to(m->slots, 4))
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: an array is not aligned to its element", who);
+    if (!m->slots && (m->state || m->history) && m->n_slots < S)
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: %u jobs but %u slots", who, S, m->n_slots);
+    a = SsmArgs();
+    a.xbc = m->xbc; a.dt = m->dt; a.z = m->z; a.y = m->y;
+    a.xbc_stride = m->xbc_stride; a.dt_stride = m->dt_stride; a.z_stride = m->z_stride; a.y_stride = m->y_stride;
+    a.A = m->A; a.skip = m->skip; a.dt_bias = m->dt_bias; a.conv_w = m->conv_w; a.conv_b = m->conv_b;
+    a.history = m->history; a.state = m->state; a.slots = m->slots;
+    a.S = S; a.n_slots = m->n_slots; a.D = (uint32_t)D; a.N = (uint32_t)N; a.G = (uint32_t)G; a.W = m->conv_width;
+    a.rows = (uint32_t)rows;
+    return SJA_OK;
+}
+
+template <typename T>
+sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
+    if (a.T > 0) {
+        const SsmShape sh = ssm_shape(a.N);
+        const uint32_t Dg = a.D / a.G, unit = sh.channels();
+        const uint32_t need = (Dg + unit - 1u) / unit;                 // warps of one group's channels
+        // the widest CTA that leaves the fewest warps without a channel (they share the tile of B and C)
+        uint32_t warps = 4u;
+        while (warps > 1u && (need + warps - 1u) / warps * warps > (need + warps / 2u - 1u) / (warps / 2u) * (warps / 2u)) warps /= 2u;
+        const uint32_t tiles = (need + warps - 1u) / warps * a.G;
+        const uint64_t all = (uint64_t)need * a.G;
+        uint64_t n_seg = std::max<uint64_t>(1, (uint64_t)c->n_sm * 8u / all);
+        n_seg = std::min<uint64_t>(n_seg, (a.T + 63u) / 64u);
+        if (n_seg < 3u && a.S == 1u) n_seg = 1u;                       // both passes over half the tokens gain nothing
+        n_seg = std::min<uint64_t>(n_seg, 65535u);
+        a.seg_len = (a.T + n_seg - 1u) / n_seg;
+        a.n_seg = (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
+        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len / 4u, 0x7FFFFFFFu);
+        if (a.n_seg > 1u) {
+            const size_t DN = (size_t)a.D * a.N, n = a.n_seg;
+            const size_t h = n * DN * 4u, f = a.resume && a.state ? h : 0u, s = n * a.D * 4u;
+            TRY(reserve(c, c->ssm_ws, h + f + s + n * 4u));
+            char* w = c->ssm_ws.as<char>();
+            a.seg_h = reinterpret_cast<float*>(w);
+            a.seg_first = reinterpret_cast<float*>(w + h);
+            a.seg_sdt = reinterpret_cast<float*>(w + h + f);
+            a.seg_flag = reinterpret_cast<uint32_t*>(w + h + f + s);
+            launch_ssm_prompt<T, true>(sh, dim3(tiles, a.n_seg - 1u), warps * 32u, c->stream, a);
+            launch_dep(ssm_carry_kernel, dim3((uint32_t)((DN + 255u) / 256u)), 256, 0, c->stream, a);
+        }
+        launch_ssm_prompt<T, false>(sh, dim3(tiles, a.n_seg), warps * 32u, c->stream, a);
+    }
+    if (a.state || (a.W > 1u && a.history))
+        launch_dep(ssm_history_kernel<T>, dim3(a.S, (a.rows + 1023u) / 1024u), 256, 0, c->stream, a);
+    CU(cudaGetLastError());
+    return SJA_OK;
+}
+
+template <typename T>
+sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
+    uint32_t lanes = 1u;
+    while (lanes * 4u < a.N) lanes *= 2u;
+    const uint32_t vec = a.N % 4u == 0u && aligned16(a.A) && aligned16(a.state) ? 1u : 0u;
+    const size_t smem = (size_t)2u * a.G * lanes * 4u * sizeof(float);
+    // few jobs: up to eight CTAs share one job's channels
+    const uint32_t per = SSM_STEP_THREADS / lanes;
+    uint32_t ctas = 1u;
+    while (ctas < 8u && (uint64_t)a.S * ctas < 2u * (uint64_t)c->n_sm && ctas * per < a.D) ctas *= 2u;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.S * ctas);
+    cfg.blockDim = dim3(SSM_STEP_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = c->stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ctas; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    CU(cudaLaunchKernelEx(&cfg, ssm_step_kernel<T>, a, lanes, vec));
+    return SJA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+sja_status sja_ssm_prompt(sja_ctx* c, const sja_ssm* ssm, uint32_t S, uint64_t T, const uint64_t* off, uint32_t resume) {
+    TRY(check_ctx(c));
+    SsmArgs a;
+    TRY(ssm_args(c, ssm, S, T, "sja_ssm_prompt", a));
+    if (resume > 1u) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_prompt: resume must be 0 or 1");
+    if (T >= (1ull << 40)) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_prompt: too many tokens");
+    if (S == 0u && T == 0u) return SJA_OK;
+    if (S == 0u) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_prompt: tokens without a job");
+    if (!off || !aligned_to(off, 8)) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_prompt: off is NULL or misaligned");
+    if (S > 0x7FFFFFFFu) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_prompt: too many jobs");
+    a.off = off; a.T = T; a.resume = resume;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return cuda_fail(c, cudaErrorInvalidDevice, "cudaSetDevice");
+    return ssm->dtype == SJA_F32 ? run_ssm_prompt<float>(c, a) : ssm->dtype == SJA_F16 ? run_ssm_prompt<__half>(c, a)
+                                                                                       : run_ssm_prompt<__nv_bfloat16>(c, a);
+}
+
+sja_status sja_ssm_step(sja_ctx* c, const sja_ssm* ssm, uint32_t S) {
+    TRY(check_ctx(c));
+    SsmArgs a;
+    TRY(ssm_args(c, ssm, S, S, "sja_ssm_step", a));
+    if (!a.state && S) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_step: state is NULL");
+    if (S > (1u << 27)) return fail(c, SJA_ERR_INVALID_ARG, "sja_ssm_step: too many jobs");
+    if (S == 0u) return SJA_OK;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return cuda_fail(c, cudaErrorInvalidDevice, "cudaSetDevice");
+    return ssm->dtype == SJA_F32 ? run_ssm_step<float>(c, a) : ssm->dtype == SJA_F16 ? run_ssm_step<__half>(c, a)
+                                                                                     : run_ssm_step<__nv_bfloat16>(c, a);
+}
+
+sja_status sja_token_stats(sja_ctx* c, const sja_token_rows* m) {
+    TRY(check_ctx(c));
+    if (!m) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: rows is NULL");
+    if (m->dtype > SJA_BF16) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: unknown dtype %u", m->dtype);
+    if (m->vocab < 1u || m->vocab > (1u << 30)) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: vocab %u not in 1 .. 2^30", m->vocab);
+    if (m->top > TOK_MAX_TOP) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: top %u not in 0 .. 32", m->top);
+    if (!(m->scale > 0.0f) || m->scale > 1e30f) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: scale must be positive and finite");
+    if (m->n_rows > 0x7FFFFFFFull) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: too many rows");
+    if (m->row_stride < (int64_t)m->vocab) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: row_stride is shorter than a row");
+    if (m->logp && !m->tokens) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: logp needs tokens");
+    if (m->n_rows == 0) return SJA_OK;
+    if (!m->logits) return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: logits is NULL");
+    if (!aligned_to(m->logits, dtype_size(m->dtype)) || !aligned_to(m->tokens, 8) || !aligned_to(m->logp, 4) ||
+        !aligned_to(m->entropy, 4) || !aligned_to(m->top_logp, 4) || !aligned_to(m->top_ids, 4))
+        return fail(c, SJA_ERR_INVALID_ARG, "sja_token_stats: an array is not aligned to its element");
+    TokenArgs a;
+    a.logits = m->logits; a.row_stride = m->row_stride; a.R = m->n_rows; a.V = m->vocab; a.top = m->top;
+    a.scale = m->scale;
+    a.c = m->scale * LOG2E;
+    a.tokens = m->tokens; a.logp = m->logp; a.entropy = m->entropy; a.top_logp = m->top_logp; a.top_ids = m->top_ids;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return cuda_fail(c, cudaErrorInvalidDevice, "cudaSetDevice");
+    const dim3 grid((uint32_t)a.R);
+    if (m->dtype == SJA_F32) launch_dep(token_stats_kernel<float>, grid, TOK_THREADS, 0, c->stream, a);
+    else if (m->dtype == SJA_F16) launch_dep(token_stats_kernel<__half>, grid, TOK_THREADS, 0, c->stream, a);
+    else launch_dep(token_stats_kernel<__nv_bfloat16>, grid, TOK_THREADS, 0, c->stream, a);
+    CU(cudaGetLastError());
+    return SJA_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,255 @@
+"""Selective state space scan (sja_ssm_prompt, sja_ssm_step) against the same formulas in 64 bits, step by step.
+
+Tolerances are the running error bounds of tests/forecast_reference.py, plus the rounding of y to its type."""
+import numpy as np
+import pytest
+
+from tests import forecast_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def _np(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+class Case:
+    """Inputs of one layer and a set of jobs, on the GPU and in 64 bits."""
+
+    def __init__(self, lens, D, N, G=1, W=4, dtype="bfloat16", gate=True, bias=True, seed=0, n_slots=None, pad=3):
+        import torch
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        rn = lambda *s: torch.randn(*s, device="cuda", generator=g)
+        self.t, self.lens, self.D, self.N, self.G, self.W = getattr(torch, dtype), lens, D, N, G, W
+        self.dtype, self.T, self.S, self.rows = dtype, sum(lens), len(lens), D + 2 * G * N
+        wide = rn(self.T, self.rows + 2 * D + pad).to(self.t)
+        self.wide, self.xbc, self.dt = wide, wide[:, :self.rows], wide[:, self.rows:self.rows + D]
+        self.z = wide[:, self.rows + D:self.rows + 2 * D] if gate else None
+        self.A = -torch.exp(rn(D, N))
+        self.skip = rn(D) if bias else None
+        self.dt_bias = rn(D) * 2 - 2 if bias else None
+        self.conv_w = rn(self.rows, W) * 0.6 if W else None
+        self.conv_b = rn(self.rows) * 0.2 if W and bias else None
+        self.off = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), device="cuda", dtype=torch.int64)
+        n_slots = n_slots or self.S
+        perm = np.random.default_rng(seed).permutation(n_slots)[:self.S]
+        self.slots = torch.tensor(perm, device="cuda", dtype=torch.int32)
+        self.state = rn(n_slots, D, N)
+        self.history = rn(n_slots, max(W - 1, 0), self.rows).to(self.t)
+
+    def layer(self, ctx):
+        return ctx.ssm_layer(self.A, conv_w=self.conv_w, conv_b=self.conv_b, skip=self.skip, dt_bias=self.dt_bias, n_groups=self.G)
+
+    def want(self, resume, off=None):
+        zero = lambda v, n: np.zeros(n) if v is None else _np(v)
+        perm = self.slots.cpu().numpy()
+        st, hi = _np(self.state)[perm], _np(self.history)[perm]
+        if not resume:
+            st, hi = np.zeros_like(st), np.zeros_like(hi)
+        return ref.ssm(_np(self.xbc), _np(self.dt), _np(self.z), self.off.cpu().numpy() if off is None else off, _np(self.A),
+                       zero(self.skip, self.D), zero(self.dt_bias, self.D), _np(self.conv_w), zero(self.conv_b, self.rows),
+                       self.G, st, hi)
+
+    def check(self, y, state, history, want):
+        wy, ey, ws, es, wh = want
+        perm = self.slots.cpu().numpy()
+        bound = ey + np.abs(wy) * ref.ROUND[self.dtype] + ref.TINY[self.dtype]
+        bad = np.abs(_np(y) - wy) > bound
+        assert not bad.any(), ("y", np.argwhere(bad)[:5], (np.abs(_np(y) - wy) / bound).max())
+        bad = np.abs(_np(state)[perm] - ws) > es
+        assert not bad.any(), ("state", np.argwhere(bad)[:5], (np.abs(_np(state)[perm] - ws) / es).max())
+        if self.W > 1:
+            assert np.array_equal(_np(history)[perm], wh)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2509_19086_b200 import binding
+    with binding.Sja() as c:
+        yield c
+
+
+SHAPES = [
+    # lens, D, N, G, W
+    ([1], 1, 1, 1, 1),
+    ([5], 3, 2, 3, 2),
+    ([0, 1, 2, 0, 3, 4, 5, 0], 32, 16, 1, 4),
+    ([37, 1, 64, 33], 70, 16, 1, 4),
+    ([300], 64, 16, 1, 4),
+    ([129, 700, 3, 0, 0, 250, 64], 66, 16, 2, 3),
+    ([90, 40, 200], 45, 12, 3, 4),
+    ([210, 5], 40, 8, 1, 0),
+    ([150, 31, 32], 24, 31, 1, 4),
+    ([33, 260], 20, 64, 2, 2),
+    ([97, 200], 18, 100, 1, 4),
+    ([260, 40], 9, 128, 1, 3),
+    ([50, 20], 600, 16, 4, 4),
+]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"T{sum(s[0])}-D{s[1]}-N{s[2]}-G{s[3]}-W{s[4]}")
+def test_prompt(ctx, shape, dtype):
+    lens, D, N, G, W = shape
+    for resume in (False, True):
+        c = Case(lens, D, N, G, W, dtype, gate=resume == (D % 2 == 0), bias=N != 8, seed=D + N, n_slots=len(lens) + 3)
+        want, before = c.want(resume), (c.state.clone(), c.history.clone())
+        y = c.layer(ctx).prompt(c.xbc, c.dt, c.off, state=c.state, history=c.history, z=c.z, slots=c.slots, resume=resume)
+        c.check(y, c.state, c.history, want)
+        # slots of no job stay as they were
+        rest = np.setdiff1d(np.arange(len(lens) + 3), c.slots.cpu().numpy())
+        assert (c.state[rest] == before[0][rest]).all() and (c.history[rest] == before[1][rest]).all()
+
+
+def test_prompt_is_deterministic_and_one_job_does_not_depend_on_the_others(ctx):
+    import torch
+    c = Case([400, 900, 77], 64, 16, seed=3, dtype="float32")
+    runs = []
+    for _ in range(2):
+        st, hi = c.state.clone(), c.history.clone()
+        runs.append((c.layer(ctx).prompt(c.xbc, c.dt, c.off, state=st, history=hi, z=c.z, slots=c.slots, resume=True), st, hi))
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    # what is not a number in the second job stays there
+    c.wide[500, 3], c.wide[700, c.rows + 5], c.state[c.slots[1].item(), 7, 2] = float("inf"), float("nan"), float("nan")
+    y = c.layer(ctx).prompt(c.xbc, c.dt, c.off, state=c.state, history=c.history, z=c.z, slots=c.slots, resume=True)
+    assert torch.isnan(y[400:1300]).any() and torch.isfinite(y[:400]).all() and torch.isfinite(y[1300:]).all()
+    err = (y[:400] - runs[0][0][:400]).abs().max()
+    assert err <= 1e-4 * runs[0][0][:400].abs().max()
+
+
+def test_prompt_in_pieces_and_by_single_tokens(ctx):
+    """A history in two calls, then token by token, against one pass in 64 bits."""
+    import torch
+    c = Case([60, 60, 60], 50, 16, 2, 4, "float32", seed=9)
+    want = c.want(False)
+    layer = c.layer(ctx)
+    base = c.off[:-1]
+    y = torch.empty(c.T, c.D, device="cuda")
+    done = 0
+    for n, resume in ((2, False), (30, True)):
+        rows = (base[:, None] + torch.arange(done, done + n, device="cuda")).reshape(-1)
+        off = torch.arange(0, 3 * n + 1, n, device="cuda")
+        y[rows] = layer.prompt(c.xbc[rows], c.dt[rows], off, state=c.state, history=c.history, z=c.z[rows], slots=c.slots, resume=resume)
+        done += n
+    for t in range(done, 60):
+        rows = base + t
+        y[rows] = layer.step(c.xbc[rows], c.dt[rows], c.state, history=c.history, z=c.z[rows], slots=c.slots)
+    c.check(y, c.state, c.history, want)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1, 1), (1, 300, 16, 1, 4), (3, 70, 16, 2, 4), (5, 33, 7, 3, 2), (2, 20, 128, 1, 3),
+                                   (400, 40, 32, 1, 4), (7, 500, 64, 4, 0), (2, 9, 3, 1, 4)], ids=str)
+def test_step(ctx, shape, dtype):
+    S, D, N, G, W = shape
+    c = Case([1] * S, D, N, G, W, dtype, gate=D % 2 == 0, seed=S + D, n_slots=S + 2)
+    want, before = c.want(True), c.state.clone()
+    y = c.layer(ctx).step(c.xbc, c.dt, c.state, history=c.history, z=c.z, slots=c.slots)
+    c.check(y, c.state, c.history, want)
+    rest = np.setdiff1d(np.arange(S + 2), c.slots.cpu().numpy())
+    assert (c.state[rest] == before[rest]).all()
+
+
+def test_jobs_outside_the_pool_start_from_zero_and_are_not_kept(ctx):
+    import torch
+    c = Case([40, 30, 20], 34, 16, dtype="float32", seed=4, n_slots=3)
+    slots = torch.tensor([-1, 1, 3], device="cuda", dtype=torch.int32)
+    zero_y = c.want(False)[0]
+    st, hi = c.state.clone(), c.history.clone()
+    y = c.layer(ctx).prompt(c.xbc, c.dt, c.off, state=st, history=hi, z=c.z, slots=slots, resume=True)
+    for a, b in ((0, 40), (70, 90)):
+        assert np.allclose(_np(y)[a:b], zero_y[a:b], rtol=1e-4, atol=1e-4)
+    assert torch.equal(st[[0, 2]], c.state[[0, 2]]) and torch.equal(hi[[0, 2]], c.history[[0, 2]])
+    st2, hi2 = c.state.clone(), c.history.clone()
+    c.layer(ctx).step(c.xbc[:3], c.dt[:3], st2, history=hi2, z=c.z[:3], slots=slots)
+    assert torch.equal(st2[[0, 2]], c.state[[0, 2]]) and torch.equal(hi2[[0, 2]], c.history[[0, 2]])
+    assert not torch.equal(st2[1], c.state[1])
+
+
+def test_rows_that_the_offsets_do_not_cover_stay_unwritten(ctx):
+    import torch
+    c = Case([100, 60], 32, 16, dtype="float32", seed=5)
+    out = torch.full((c.T, c.D), 7.5, device="cuda")
+    off = torch.tensor([0, 90, 140], device="cuda")
+    c.layer(ctx).prompt(c.xbc, c.dt, off, z=c.z, out=out)
+    assert (out[140:] == 7.5).all() and not (out[:140] == 7.5).any()
+    # no tokens at all: the slots hold zeros afterwards, or stay as they are
+    st, hi = c.state.clone(), c.history.clone()
+    none = torch.zeros(3, device="cuda", dtype=torch.int64)
+    c.layer(ctx).prompt(c.xbc[:0], c.dt[:0], none, state=st, history=hi, z=c.z[:0], slots=c.slots, resume=True)
+    assert torch.equal(st, c.state) and torch.equal(hi, c.history)
+    c.layer(ctx).prompt(c.xbc[:0], c.dt[:0], none, state=st, history=hi, z=c.z[:0], slots=c.slots)
+    assert not st.any() and not hi.any()
+
+
+def test_another_stream(ctx):
+    import torch
+    from paper_2509_19086_b200 import binding
+    c = Case([200, 300], 64, 16, dtype="float32", seed=6)
+    want = c.want(False)
+    side = torch.cuda.Stream()
+    with binding.Sja(stream=side.cuda_stream) as other:
+        side.wait_stream(torch.cuda.current_stream())
+        y = c.layer(other).prompt(c.xbc, c.dt, c.off, state=c.state, history=c.history, z=c.z, slots=c.slots)
+        torch.cuda.current_stream().wait_stream(side)
+        c.check(y, c.state, c.history, want)
+
+
+def test_refusals(ctx):
+    import torch
+    from paper_2509_19086_b200 import binding
+    c = Case([20, 10], 32, 16, dtype="float32", seed=7)
+    layer = c.layer(ctx)
+    ok = dict(state=c.state, history=c.history, z=c.z, slots=c.slots)
+    for kind, call in (
+        (TypeError, lambda: layer.prompt(c.xbc.cpu(), c.dt, c.off, **ok)),
+        (TypeError, lambda: layer.prompt(c.xbc.double(), c.dt, c.off, **ok)),
+        (TypeError, lambda: layer.prompt(c.xbc, c.dt.half(), c.off, **ok)),
+        (TypeError, lambda: layer.prompt(c.xbc, c.dt, c.off.int(), **ok)),
+        (TypeError, lambda: layer.prompt(c.xbc, c.dt, c.off, **dict(ok, slots=c.slots.long()))),
+        (TypeError, lambda: layer.prompt(c.xbc, c.dt, c.off, **dict(ok, state=c.state.half()))),
+        (ValueError, lambda: layer.prompt(c.xbc[:, 1:], c.dt, c.off, **ok)),
+        (ValueError, lambda: layer.prompt(c.xbc, c.dt[:5], c.off, **ok)),
+        (ValueError, lambda: layer.prompt(c.xbc, c.wide[:, ::2][:, :32], c.off, **ok)),
+        (ValueError, lambda: layer.prompt(c.xbc, c.dt, c.off, **dict(ok, state=c.state[:, :, :8]))),
+        (ValueError, lambda: layer.prompt(c.xbc, c.dt, c.off, **dict(ok, history=c.history[:, :2]))),
+        (ValueError, lambda: layer.prompt(c.xbc, c.dt, c.off, **dict(ok, slots=c.slots[:1]))),
+        (ValueError, lambda: ctx.ssm_layer(c.A, conv_w=c.conv_w[:-1])),
+        (ValueError, lambda: ctx.ssm_layer(c.A, n_groups=5)),
+        (binding.SjaError, lambda: ctx.ssm_layer(torch.zeros(4, 129, device="cuda")).step(
+            torch.zeros(1, 262, device="cuda"), torch.zeros(1, 4, device="cuda"), torch.zeros(1, 4, 129, device="cuda"))),
+        (binding.SjaError, lambda: layer.prompt(c.xbc, c.dt, c.off, state=c.state[:1], z=c.z)),
+        (binding.SjaError, lambda: layer.prompt(c.xbc, c.dt, c.off[:1])),
+        (binding.SjaError, lambda: layer.prompt(c.xbc[:1].expand(30, -1), c.dt, c.off)),
+    ):
+        with pytest.raises(kind):
+            call()
+    a, _ = layer._fill(c.xbc, c.dt, c.z, c.state, c.history, c.slots, 2, None)
+    import ctypes
+    lib = binding.load_library()
+    for field, value in (("dtype", 3), ("n_groups", 0), ("n_state", 0), ("conv_width", 5), ("conv_width", 0), ("A", None),
+                         ("xbc", None), ("y_stride", 31), ("dt", a.dt + 2), ("state", a.state + 1)):
+        b = binding.SjaSsm.from_buffer_copy(a)
+        setattr(b, field, value)
+        assert lib.sja_ssm_prompt(ctx._h, ctypes.byref(b), 2, c.T, c.off.data_ptr(), 0) == 1, field
+        assert lib.sja_last_error(ctx._h)
+    assert lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), 2, c.T, c.off.data_ptr(), 2) == 1
+    assert lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), 2, c.T, None, 0) == 1
+    a.state = None
+    assert lib.sja_ssm_step(ctx._h, ctypes.byref(a), 2) == 1
+
+
+def test_failed_workspace_leaves_a_usable_context():
+    from paper_2509_19086_b200 import binding
+    with binding.Sja() as fresh:
+        c = Case([2000], 64, 16, dtype="float32", seed=8)
+        want = c.want(False)
+        fresh.debug_fail_alloc(1)
+        before = c.state.clone()
+        with pytest.raises(binding.SjaError) as e:
+            c.layer(fresh).prompt(c.xbc, c.dt, c.off, state=c.state, history=c.history, z=c.z, slots=c.slots)
+        assert e.value.status == 5 and (c.state == before).all()
+        y = c.layer(fresh).prompt(c.xbc, c.dt, c.off, state=c.state, history=c.history, z=c.z, slots=c.slots)
+        c.check(y, c.state, c.history, want)

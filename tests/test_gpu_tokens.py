@@ -1,0 +1,131 @@
+"""Token statistics (sja_token_stats) against the definition in 64 bits: whole numbers equal, log probabilities and
+entropies within the rounding bound of tests/forecast_reference.py."""
+import numpy as np
+import pytest
+
+from tests import forecast_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2509_19086_b200 import binding
+    with binding.Sja() as c:
+        yield c
+
+
+def _check(ctx, logits, tokens, top, scale=1.0):
+    import torch
+    tok = torch.as_tensor(np.asarray(tokens, dtype=np.int64), device="cuda")
+    got = {k: v.cpu().numpy() for k, v in ctx.token_stats(logits, tok, top=top, scale=scale).items()}
+    logp, entropy, top_logp, top_ids, bound = ref.token_stats(logits.double().cpu().numpy(), tokens, top, scale)
+    assert np.array_equal(got["top_ids"], top_ids)
+    for name, want, b in (("logp", logp, bound), ("entropy", entropy, bound), ("top_logp", top_logp, bound[:, None])):
+        g, b = got[name].astype(np.float64), np.broadcast_to(b, want.shape)
+        fine = np.isfinite(want)
+        assert np.array_equal(g[~fine], want[~fine], equal_nan=True), name
+        off = np.abs(g - np.where(fine, want, 0.0))
+        assert (off[fine] <= b[fine]).all(), (name, (off[fine] / b[fine]).max())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("V", [1, 2, 7, 31, 32, 33, 64, 100, 255, 1000, 1024, 1025, 2047, 2049, 4096, 9001, 50001, 131072])
+def test_sizes(ctx, V, dtype):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V)
+    R = 3 if V > 4096 else 13
+    for top, scale, pad, masked in ((0, 1.0, 0, 0.0), (1, 0.7, 1, 0.0), (5, 1.0, 8, 0.5), (32, 1.9, 3, 0.97)):
+        wide = (torch.randn(R, V + pad, device="cuda", generator=g) * 3).to(getattr(torch, dtype))
+        x = wide[:, pad // 2:pad // 2 + V]
+        x[torch.rand(R, V, device="cuda", generator=g) < masked] = -float("inf")
+        tokens = np.random.default_rng(V).integers(0, V, R)
+        tokens[0] = -1
+        _check(ctx, x, tokens, top, scale)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 5, 40, 300, 700])
+@pytest.mark.parametrize("V", [600, 20000])
+def test_rows(ctx, rows, V):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x = (torch.randn(rows, V, device="cuda", generator=g) * 2).bfloat16()
+    _check(ctx, x, np.random.default_rng(1).integers(0, V, rows), 9)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("V", [5, 40, 1000, 3000, 40000])
+def test_rows_that_are_hard_to_order(ctx, V, dtype):
+    """Ties, rows of one value, empty rows, a few entries left by a mask, values gathered in one place, -0, NaN, +inf."""
+    import torch
+    t = getattr(torch, dtype)
+    rng = np.random.default_rng(V)
+    x = torch.zeros(16, V, device="cuda", dtype=t)
+    x[1] = -float("inf")
+    x[2] = torch.as_tensor(rng.integers(0, 3, V), device="cuda")
+    x[3] = -float("inf")
+    x[3, V // 2], x[3, V - 1] = 2.0, 2.0
+    x[4] = torch.arange(V, device="cuda") % 97
+    x[5] = torch.linspace(-30, 30, V, device="cuda")
+    x[6] = torch.linspace(30, -30, V, device="cuda")
+    x[7, ::2] = -0.0
+    x[8], x[8, V // 3] = 1.5, float("nan")
+    x[9, V // 2] = float("inf")
+    x[10] = float("nan")
+    x[11] = torch.finfo(t).min
+    x[11, V // 4] = 3.0
+    # every warp but one of a 256-thread sweep over vectors holds the large values
+    at = torch.arange(V, device="cuda")
+    x[12] = torch.where((at // 8) % 256 < 32, torch.full_like(at, -60000, dtype=torch.float32), torch.as_tensor(rng.normal(size=V), device="cuda").float()).to(t)
+    x[13] = torch.where((at // 4) % 256 < 32, torch.full_like(at, -float("inf"), dtype=torch.float32), torch.as_tensor(rng.normal(size=V), device="cuda").float()).to(t)
+    x[14] = torch.where(at < V // 2, -float("inf"), at.float() % 50).to(t)
+    x[15] = -float("inf")
+    x[15, 0] = torch.finfo(t).min
+    for top in (1, 4, 32):
+        _check(ctx, x, np.minimum(np.arange(16) * 3, V - 1), top)
+
+
+def test_tokens_outside_the_row_and_single_outputs(ctx):
+    import torch
+    x = torch.randn(4, 50, device="cuda")
+    tok = torch.tensor([-5, 50, 1 << 40, 0], device="cuda")
+    logp = ctx.token_stats(x, tok)["logp"].cpu().numpy()
+    assert logp[0] == 0 and np.isnan(logp[1]) and np.isnan(logp[2]) and np.isfinite(logp[3])
+    out = ctx.token_stats(x, top=3)
+    assert "logp" not in out and out["top_ids"].shape == (4, 3)
+    assert torch.equal(out["top_ids"][:, 0].long(), x.argmax(dim=1))
+    assert ctx.token_stats(x[:0], top=2)["top_ids"].shape == (0, 2)
+
+
+def test_row_offsets_beyond_32_bits(ctx):
+    """Rows apart by more than 2^31 elements in all."""
+    import torch
+    wide = torch.empty(3, 1 << 30, device="cuda", dtype=torch.float16)
+    x = wide[:, 5:1005]
+    x.copy_(torch.randn(3, 1000, device="cuda"))
+    _check(ctx, x, [1, 2, 3], 4)
+    del wide, x
+    torch.cuda.empty_cache()
+
+
+def test_refusals(ctx):
+    import torch
+    from paper_2509_19086_b200 import binding
+    x, tok = torch.randn(4, 50, device="cuda"), torch.zeros(4, device="cuda", dtype=torch.int64)
+    for kind, call in (
+        (TypeError, lambda: ctx.token_stats(x.cpu(), tok)),
+        (TypeError, lambda: ctx.token_stats(x.double(), tok)),
+        (TypeError, lambda: ctx.token_stats(x, tok.int())),
+        (ValueError, lambda: ctx.token_stats(x, tok[:3])),
+        (ValueError, lambda: ctx.token_stats(x.t(), tok)),
+        (ValueError, lambda: ctx.token_stats(x[0], tok)),
+        (binding.SjaError, lambda: ctx.token_stats(x, tok, top=33)),
+        (binding.SjaError, lambda: ctx.token_stats(x, tok, scale=0.0)),
+        (binding.SjaError, lambda: ctx.token_stats(x, tok, scale=float("nan"))),
+        (binding.SjaError, lambda: ctx.token_stats(x[:, :0], tok)),
+        (binding.SjaError, lambda: ctx.token_stats(x[:1].expand(4, -1), tok)),
+    ):
+        with pytest.raises(kind):
+            call()
