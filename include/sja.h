@@ -398,7 +398,7 @@ typedef struct {
     uint32_t dtype;              /* sja_dtype of xbc, dt, z, y and history */
     uint32_t n_channels;         /* D, 1 .. 2^20 */
     uint32_t n_state;            /* N, 1 .. 128 */
-    uint32_t n_groups;           /* G, divides D; G * N <= 4096 */
+    uint32_t n_groups;           /* G, 1 .. 32, divides D */
     uint32_t conv_width;         /* W, 0 .. 4 */
     uint32_t n_slots;            /* size of the pools */
     const float* A;              /* [D, N] */

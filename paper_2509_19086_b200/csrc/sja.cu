@@ -1456,9 +1456,9 @@ sja_status sja_get_scan(sja_ctx* c, uint64_t* boff, uint32_t* k, uint32_t* D, ui
 // Forecasting side: the recurrent scan of a sequence model, and the statistics of its answers.
 namespace {
 
-// Instance of the prompt kernel for N states: one thread holds two channels and up to 16 of their states, wider
-// states are shared by 2, 4 or 8 lanes.
-struct SsmShape { uint32_t K, lanes; uint32_t channels() const { return 32u / lanes * 2u; } };
+// Instance of the prompt kernel for N states: a lane holds up to 16 states of a channel, wider states are shared by 2,
+// 4 or 8 lanes.
+struct SsmShape { uint32_t K, lanes; uint32_t channels() const { return 32u / lanes; } };
 SsmShape ssm_shape(uint32_t N) {
     if (N <= 8u) return {8u, 1u};
     if (N <= 16u) return {16u, 1u};
@@ -1469,11 +1469,11 @@ SsmShape ssm_shape(uint32_t N) {
 
 template <typename T, bool CARRY>
 void launch_ssm_prompt(const SsmShape& sh, dim3 grid, uint32_t threads, cudaStream_t stream, const SsmArgs& a) {
-    if (sh.K == 8u) launch_dep(ssm_prompt_kernel<T, 8, 1, 2, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.lanes == 1u) launch_dep(ssm_prompt_kernel<T, 16, 1, 2, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.lanes == 2u) launch_dep(ssm_prompt_kernel<T, 16, 2, 2, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.lanes == 4u) launch_dep(ssm_prompt_kernel<T, 16, 4, 2, CARRY>, grid, threads, 0, stream, a);
-    else launch_dep(ssm_prompt_kernel<T, 16, 8, 2, CARRY>, grid, threads, 0, stream, a);
+    if (sh.K == 8u) launch_dep(ssm_prompt_kernel<T, 8, 1, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.lanes == 1u) launch_dep(ssm_prompt_kernel<T, 16, 1, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.lanes == 2u) launch_dep(ssm_prompt_kernel<T, 16, 2, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.lanes == 4u) launch_dep(ssm_prompt_kernel<T, 16, 4, CARRY>, grid, threads, 0, stream, a);
+    else launch_dep(ssm_prompt_kernel<T, 16, 8, CARRY>, grid, threads, 0, stream, a);
 }
 
 bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0; }
@@ -1486,8 +1486,8 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
     const uint64_t D = m->n_channels, N = m->n_state, G = m->n_groups;
     if (D < 1 || D > (1u << 20)) return fail(c, SJA_ERR_INVALID_ARG, "%s: n_channels %u not in 1 .. 2^20", who, m->n_channels);
     if (N < 1 || N > SSM_MAX_STATE) return fail(c, SJA_ERR_INVALID_ARG, "%s: n_state %u not in 1 .. 128", who, m->n_state);
-    if (G < 1 || D % G != 0 || G * N > 4096)
-        return fail(c, SJA_ERR_INVALID_ARG, "%s: n_groups %u must divide n_channels, with n_groups * n_state <= 4096", who, m->n_groups);
+    if (G < 1 || G > 32 || D % G != 0)
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: n_groups %u not in 1 .. 32, or no divisor of n_channels", who, m->n_groups);
     if (m->conv_width > SSM_MAX_WIDTH) return fail(c, SJA_ERR_INVALID_ARG, "%s: conv_width %u not in 0 .. 4", who, m->conv_width);
     if ((m->conv_width == 0) != (m->conv_w == nullptr))
         return fail(c, SJA_ERR_INVALID_ARG, "%s: conv_w goes with conv_width >= 1", who);
@@ -1512,6 +1512,10 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
     return SJA_OK;
 }
 
+// Warps an SM that a prompt aims at by splitting the token axis (16 of 128 registers fit).
+#ifndef SSM_WARPS_PER_SM
+#define SSM_WARPS_PER_SM 16u
+#endif
 template <typename T>
 sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
     if (a.T > 0) {
@@ -1519,17 +1523,17 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         const uint32_t Dg = a.D / a.G, unit = sh.channels();
         const uint32_t need = (Dg + unit - 1u) / unit;                 // warps of one group's channels
         // the widest CTA that leaves the fewest warps without a channel (they share the tile of B and C)
-        uint32_t warps = 4u;
+        uint32_t warps = SSM_THREADS / 32u;
         while (warps > 1u && (need + warps - 1u) / warps * warps > (need + warps / 2u - 1u) / (warps / 2u) * (warps / 2u)) warps /= 2u;
         const uint32_t tiles = (need + warps - 1u) / warps * a.G;
         const uint64_t all = (uint64_t)need * a.G;
-        uint64_t n_seg = std::max<uint64_t>(1, (uint64_t)c->n_sm * 8u / all);
-        n_seg = std::min<uint64_t>(n_seg, (a.T + 63u) / 64u);
+        uint64_t n_seg = std::max<uint64_t>(1, (uint64_t)c->n_sm * SSM_WARPS_PER_SM / all);
+        n_seg = std::min<uint64_t>(n_seg, (a.T + 31u) / 32u);
         if (n_seg < 3u && a.S == 1u) n_seg = 1u;                       // both passes over half the tokens gain nothing
         n_seg = std::min<uint64_t>(n_seg, 65535u);
         a.seg_len = (a.T + n_seg - 1u) / n_seg;
         a.n_seg = (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
-        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len / 4u, 0x7FFFFFFFu);
+        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len / 2u, 0x7FFFFFFFu);
         if (a.n_seg > 1u) {
             const size_t DN = (size_t)a.D * a.N, n = a.n_seg;
             const size_t h = n * DN * 4u, f = a.resume && a.state ? h : 0u, s = n * a.D * 4u;
@@ -1556,10 +1560,8 @@ sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
     while (lanes * 4u < a.N) lanes *= 2u;
     const uint32_t vec = a.N % 4u == 0u && aligned16(a.A) && aligned16(a.state) ? 1u : 0u;
     const size_t smem = (size_t)2u * a.G * lanes * 4u * sizeof(float);
-    // few jobs: up to eight CTAs share one job's channels
-    const uint32_t per = SSM_STEP_THREADS / lanes;
-    uint32_t ctas = 1u;
-    while (ctas < 8u && (uint64_t)a.S * ctas < 2u * (uint64_t)c->n_sm && ctas * per < a.D) ctas *= 2u;
+    // a job's channels are spread over up to eight CTAs (a portable cluster)
+    const uint32_t ctas = std::min<uint32_t>(8u, (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.S * ctas);
     cfg.blockDim = dim3(SSM_STEP_THREADS);

@@ -47,14 +47,31 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
-// log1p keeps the relative accuracy of small time steps (softplus(v) ~ e^v for very negative v)
-__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(__expf(-fabsf(v))); }
-
 __device__ __forceinline__ float exp2_fast(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+__device__ __forceinline__ float rcp_fast(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+constexpr float LN2 = 0.693147182f, LOG2E = 1.44269504f;
+
+__device__ __forceinline__ float silu(float v) { return v * rcp_fast(1.0f + exp2_fast(-LOG2E * v)); }
+
+// softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|).  Time steps of 0.001 and less come from very negative v, where
+// log(1 + e) would lose what 1 + e rounds away; log1p(e) = 2 atanh(q), q = e / (2 + e) in 0 .. 1/3, keeps it: the
+// odd series in q, its even part fitted by a polynomial in q^2 on 0 .. 1/9 (relative error 8e-9).
+__device__ __forceinline__ float softplus(float v) {
+    const float e = exp2_fast(-LOG2E * fabsf(v)), q = e * rcp_fast(2.0f + e), w = q * q;
+    float p = fmaf(w, 0.140873283f, 0.139807090f);
+    p = fmaf(w, p, 0.200124264f);
+    p = fmaf(w, p, 0.333331585f);
+    p = fmaf(w, p, 1.0f);
+    return fmaf(q + q, p, fmaxf(v, 0.0f));
 }
 
 // Two 32-bit values in one 64-bit register pair: one instruction issued for two multiply-adds.
@@ -156,32 +173,31 @@ struct Conv {
     }
 };
 
-__host__ __device__ constexpr int ssm_tile_tokens(int np) { return np <= 32 ? 32 : np <= 64 ? 16 : 8; }
+constexpr uint32_t SSM_THREADS = 256;    // most threads of a prompt CTA
+// Tokens whose B and C one CTA keeps at a time: a thread convolves a stretch of 8 tokens of one column (2 NP of them).
+__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np <= 32u ? 32u : 1024u / np; }
 
-// Prompts.  A thread owns CPT channels and K of their states (LPC lanes share a channel), walks its segment of the
-// token axis and keeps the states in registers; B and C of a tile of tokens are convolved once per CTA into shared
-// memory and read by broadcast.  CARRY = true is the first pass of a split: what the job that crosses the segment's
-// end adds to its state inside the segment, and its sum of time steps (exp(A sum dt) is the decay over the segment).
-template <typename T, int K, int LPC, int CPT, bool CARRY>
-__global__ void __launch_bounds__(128) ssm_prompt_kernel(const SsmArgs a) {
-    constexpr int NP = K * LPC, TT = ssm_tile_tokens(NP), CPW = 32 / LPC, U = 4;
-    __shared__ __align__(16) float sB[TT * NP], sC[TT * NP];
+// Prompts.  A thread owns one channel and K of its states (LPC lanes share a channel), walks its segment of the token
+// axis and keeps the states in registers.  B and C of a tile of tokens are convolved once per CTA into shared memory,
+// one tile ahead of the walk, and read by broadcast; x, dt and z of the next four tokens are on their way while four
+// are worked on.  CARRY = true is the first pass of a split: what the job that crosses the segment's end adds to its
+// state inside the segment, and its sum of time steps (exp(A sum dt) is the decay over the segment).
+template <typename T, int K, int LPC, bool CARRY>
+__global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArgs a) {
+    constexpr uint32_t NP = K * LPC, TT = ssm_tile_tokens(NP), CPW = 32 / LPC, COLS = CARRY ? NP : 2 * NP;
+    constexpr int U = 4, STRETCH = 8;
+    __shared__ __align__(16) float s_bc[2][TT * 2 * NP];       // [buffer][token][B | C]
     dep_wait();
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
-    const uint32_t Dg = a.D / a.G, span = (blockDim.x >> 5) * CPW * CPT;
+    const uint32_t Dg = a.D / a.G, span = (blockDim.x >> 5) * CPW;
     const uint32_t tiles = (Dg + span - 1u) / span;
     const uint32_t g = blockIdx.x / tiles, seg = blockIdx.y;
-    const uint32_t in_group = (blockIdx.x % tiles) * span + warp * (CPW * CPT) + lane / LPC;
+    const uint32_t in_group = (blockIdx.x % tiles) * span + warp * CPW + lane / LPC;
     const uint32_t n0 = (lane % LPC) * K;
-    uint32_t ch[CPT];
-    bool live[CPT];
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-        live[i] = in_group + i * CPW < Dg;
-        ch[i] = g * Dg + (live[i] ? in_group + i * CPW : 0u);
-    }
+    const bool live = in_group < Dg;
+    const uint32_t ch = g * Dg + (live ? in_group : 0u);
     const uint64_t b0 = segment_bound(a, seg), b1 = segment_bound(a, seg + 1u);
-    uint64_t begin = b0;
+    uint64_t t = b0;
     uint32_t s;
     if (CARRY) {
         s = warp_lower_bound(a.off, a.S + 1u, b1 + 1ull);
@@ -190,59 +206,66 @@ __global__ void __launch_bounds__(128) ssm_prompt_kernel(const SsmArgs a) {
         const uint32_t flag = (s >= a.S || q >= b1) ? SEG_NONE : q >= b0 ? SEG_STARTS : SEG_PASSES;
         if (blockIdx.x == 0u && tid == 0u) a.seg_flag[seg] = flag;
         if (flag == SEG_NONE) return;
-        begin = q > b0 ? q : b0;
+        t = q > b0 ? q : b0;
     } else {
         s = warp_lower_bound(a.off, a.S + 1u, b0 + 1ull);
         s = s ? s - 1u : 0u;
     }
 
-    F2 A2[CPT][K / 2], h[CPT][K / 2];
-    Conv cx[CPT];
-    float skip[CPT], bias[CPT], sdt[CPT];
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-        cx[i].load(a, ch[i]);
-        skip[i] = a.skip ? a.skip[ch[i]] : 0.0f;
-        bias[i] = a.dt_bias ? a.dt_bias[ch[i]] : 0.0f;
-        sdt[i] = 0.0f;
+    F2 A2[K / 2], h[K / 2];
+    Conv cx;
+    cx.load(a, ch);
+    const float skip = a.skip ? a.skip[ch] : 0.0f, bias = a.dt_bias ? a.dt_bias[ch] : 0.0f;
+    float sdt = 0.0f;
+    auto load_states = [&](F2 (&to)[K / 2], const float* from, float scale) {
+        const float* r = from + (uint64_t)ch * a.N;
 #pragma unroll
         for (int k = 0; k < K / 2; ++k) {
             const uint32_t n = n0 + 2 * k;
-            const float* r = a.A + (uint64_t)ch[i] * a.N;
-            A2[i][k] = f2(n < a.N ? r[n] * 1.44269504f : 0.0f, n + 1u < a.N ? r[n + 1u] * 1.44269504f : 0.0f);
-            h[i][k] = f2(0.0f, 0.0f);
+            to[k] = f2(n < a.N ? r[n] * scale : 0.0f, n + 1u < a.N ? r[n + 1u] * scale : 0.0f);
         }
-    }
-    auto load_h = [&](const float* from) {
-#pragma unroll
-        for (int i = 0; i < CPT; ++i)
-#pragma unroll
-            for (int k = 0; k < K / 2; ++k) {
-                const uint32_t n = n0 + 2 * k;
-                const float* r = from + (uint64_t)ch[i] * a.N;
-                h[i][k] = f2(n < a.N ? r[n] : 0.0f, n + 1u < a.N ? r[n + 1u] : 0.0f);
-            }
     };
     auto store_h = [&](float* to) {
+        float* r = to + (uint64_t)ch * a.N;
 #pragma unroll
-        for (int i = 0; i < CPT; ++i)
-#pragma unroll
-            for (int k = 0; k < K / 2; ++k) {
-                const uint32_t n = n0 + 2 * k;
-                float* r = to + (uint64_t)ch[i] * a.N;
-                float v0, v1;
-                f2_split(h[i][k], v0, v1);
-                if (live[i] && n < a.N) r[n] = v0;
-                if (live[i] && n + 1u < a.N) r[n + 1u] = v1;
-            }
+        for (int k = 0; k < K / 2; ++k) {
+            const uint32_t n = n0 + 2 * k;
+            float v0, v1;
+            f2_split(h[k], v0, v1);
+            if (live && n < a.N) r[n] = v0;
+            if (live && n + 1u < a.N) r[n + 1u] = v1;
+        }
     };
+    load_states(A2, a.A, LOG2E);
+#pragma unroll
+    for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
     const uint64_t DN = (uint64_t)a.D * a.N;
     const T* xp = static_cast<const T*>(a.xbc);
-    const T* dp = static_cast<const T*>(a.dt);
-    const T* zp = static_cast<const T*>(a.z);
-    T* yp = static_cast<T*>(a.y);
 
-    uint64_t t = begin;
+    // this thread's part in convolving B and C: column bc_col, tokens bc_from .. bc_from + 7 of a tile
+    const uint32_t parts = max(blockDim.x / COLS, 1u), tile_tok = min(parts * (uint32_t)STRETCH, TT);
+    auto stage = [&](uint32_t w, uint64_t q, int64_t slot, uint64_t at, uint32_t n_tok, float* to) {
+        const uint32_t col = w % COLS, from = (w / COLS) * STRETCH, n = col % NP;
+        if (from >= n_tok) return;
+        const uint32_t cnt = min((uint32_t)STRETCH, n_tok - from);
+        float* dst = to + from * (2 * NP) + (col < NP ? 0u : NP) + n;
+        if (n >= a.N) {
+#pragma unroll
+            for (int i = 0; i < STRETCH; ++i) dst[i * (2 * NP)] = 0.0f;      // the tile has room for whole stretches
+            return;
+        }
+        const uint32_t rc = a.D + (col < NP ? 0u : a.G * a.N) + g * a.N + n;
+        Conv cv;
+        cv.load(a, rc);
+        cv.template seek<T>(a, q, (int64_t)(at - q) + from, rc, slot);
+        const T* src = xp + (int64_t)(at + from) * a.xbc_stride + rc;
+        float v[STRETCH];
+#pragma unroll
+        for (int i = 0; i < STRETCH; ++i) v[i] = (uint32_t)i < cnt ? to_f32(src[(int64_t)i * a.xbc_stride]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < STRETCH; ++i) dst[i * (2 * NP)] = cv.next(a.W, v[i]);
+    };
+
     for (; t < b1 && s < a.S; ++s) {
         const uint64_t q = a.off[s];
         uint64_t e = a.off[s + 1u];
@@ -252,114 +275,101 @@ __global__ void __launch_bounds__(128) ssm_prompt_kernel(const SsmArgs a) {
         const int64_t slot = slot_of(a, s);
         // where the job's state comes from: the segment before, its slot, or nothing
         if (q < t) {
-            if (!CARRY) load_h(a.seg_h + (uint64_t)(seg - 1u) * DN);
+            if (!CARRY) load_states(h, a.seg_h + (uint64_t)(seg - 1u) * DN, 1.0f);
         } else if (a.resume && slot >= 0 && a.state) {
             // a job that goes on behind this segment may be stored by another CTA meanwhile: the first pass kept a copy
-            if (CARRY || ends || a.n_seg == 1u) load_h(a.state + slot * (int64_t)DN);
-            else load_h(a.seg_first + (uint64_t)seg * DN);
+            if (CARRY || ends || a.n_seg == 1u) load_states(h, a.state + slot * (int64_t)DN, 1.0f);
+            else load_states(h, a.seg_first + (uint64_t)seg * DN, 1.0f);
             if (CARRY) store_h(a.seg_first + (uint64_t)seg * DN);
         } else {
 #pragma unroll
-            for (int i = 0; i < CPT; ++i)
-#pragma unroll
-                for (int k = 0; k < K / 2; ++k) h[i][k] = f2(0.0f, 0.0f);
+            for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
         }
+        cx.template seek<T>(a, q, (int64_t)(t - q), ch, slot);
+        const T* px = xp + (int64_t)t * a.xbc_stride + ch;
+        const T* pd = static_cast<const T*>(a.dt) + (int64_t)t * a.dt_stride + ch;
+        const T* pz = a.z && !CARRY ? static_cast<const T*>(a.z) + (int64_t)t * a.z_stride + ch : nullptr;
+        T* py = static_cast<T*>(a.y) + (int64_t)t * a.y_stride + ch;
+        uint64_t left = e - t;
+        T xr[U], dr[U], zr[U];
+        auto fetch = [&](uint64_t have) {              // rows behind the job's end are not touched
 #pragma unroll
-        for (int i = 0; i < CPT; ++i) cx[i].template seek<T>(a, q, (int64_t)(t - q), ch[i], slot);
-
-        while (t < e) {
-            const uint32_t n_tok = e - t < (uint64_t)TT ? (uint32_t)(e - t) : (uint32_t)TT;
-            __syncthreads();
-            // convolve B (and C) of the tile: a thread takes one column and every fourth stretch of tokens
-            const uint32_t cols = CARRY ? NP : 2 * NP;
-            const uint32_t parts = blockDim.x / cols ? blockDim.x / cols : 1u, per = (n_tok + parts - 1u) / parts;
-            for (uint32_t w = tid; w < cols * parts; w += blockDim.x) {
-                const uint32_t col = w % cols, from = (w / cols) * per, to = min(from + per, n_tok);
-                const uint32_t n = col % NP;
-                float* dst = col < NP ? sB : sC;
-                if (n >= a.N) {
-                    for (uint32_t i = from; i < to; ++i) dst[i * NP + n] = 0.0f;
-                } else if (from < to) {
-                    const uint32_t rc = a.D + (col < NP ? 0u : a.G * a.N) + g * a.N + n;
-                    Conv cv;
-                    cv.load(a, rc);
-                    cv.template seek<T>(a, q, (int64_t)(t - q) + from, rc, slot);
-                    for (uint32_t i = from; i < to; ++i)
-                        dst[i * NP + n] = cv.next(a.W, to_f32(xp[(int64_t)(t + i) * a.xbc_stride + rc]));
+            for (int j = 0; j < U; ++j) {
+                if ((uint64_t)j < have) {
+                    xr[j] = px[j * a.xbc_stride];
+                    dr[j] = pd[j * a.dt_stride];
+                    if (pz) zr[j] = pz[j * a.z_stride];
                 }
             }
+        };
+#pragma unroll
+        for (int j = 0; j < U; ++j) xr[j] = dr[j] = zr[j] = from_f32<T>(0.0f);
+        fetch(left);
+        uint32_t buf = 0;
+        __syncthreads();
+        for (uint32_t w = tid; w < COLS * parts; w += blockDim.x)
+            stage(w, q, slot, t, (uint32_t)min((uint64_t)tile_tok, left), s_bc[0]);
+        while (t < e) {
+            const uint32_t n_tok = (uint32_t)min((uint64_t)tile_tok, left);
             __syncthreads();
+            if (left > n_tok)
+                for (uint32_t w = tid; w < COLS * parts; w += blockDim.x)
+                    stage(w, q, slot, t + n_tok, (uint32_t)min((uint64_t)tile_tok, left - n_tok), s_bc[buf ^ 1u]);
+            const float* bc = s_bc[buf] + n0;
             for (uint32_t i0 = 0; i0 < n_tok; i0 += U) {
-                float xv[U][CPT], dv[U][CPT], zv[U][CPT];
+                float xv[U], dv[U], zv[U];
 #pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    const uint64_t r = t + min(i0 + j, n_tok - 1u);
-#pragma unroll
-                    for (int i = 0; i < CPT; ++i) {
-                        xv[j][i] = to_f32(xp[(int64_t)r * a.xbc_stride + ch[i]]);
-                        dv[j][i] = to_f32(dp[(int64_t)r * a.dt_stride + ch[i]]);
-                        zv[j][i] = !CARRY && zp ? to_f32(zp[(int64_t)r * a.z_stride + ch[i]]) : 0.0f;
-                    }
-                }
+                for (int j = 0; j < U; ++j) { xv[j] = to_f32(xr[j]); dv[j] = to_f32(dr[j]); zv[j] = to_f32(zr[j]); }
+                px += U * a.xbc_stride; pd += U * a.dt_stride;
+                if (pz) pz += U * a.z_stride;
+                if (left > i0 + U) fetch(left - i0 - U);
 #pragma unroll
                 for (int j = 0; j < U; ++j) {
                     if (i0 + j >= n_tok) break;
-                    F2 d2[CPT], du2[CPT], acc[CPT];
-                    float u[CPT];
-#pragma unroll
-                    for (int i = 0; i < CPT; ++i) {
-                        u[i] = cx[i].next(a.W, xv[j][i]);
-                        const float d = softplus(dv[j][i] + bias[i]);
-                        if (CARRY) sdt[i] += d;
-                        d2[i] = f2(d, d);
-                        du2[i] = f2(d * u[i], d * u[i]);
-                        acc[i] = f2(0.0f, 0.0f);
-                    }
-                    const ulonglong2* pB = reinterpret_cast<const ulonglong2*>(sB + (i0 + j) * NP + n0);
-                    const ulonglong2* pC = reinterpret_cast<const ulonglong2*>(sC + (i0 + j) * NP + n0);
+                    const float u = cx.next(a.W, xv[j]), d = softplus(dv[j] + bias);
+                    if (CARRY) sdt += d;
+                    const F2 d2 = f2(d, d), du2 = f2(d * u, d * u);
+                    F2 acc = f2(0.0f, 0.0f);
+                    const ulonglong2* pB = reinterpret_cast<const ulonglong2*>(bc + (i0 + j) * (2 * NP));
 #pragma unroll
                     for (int k = 0; k < K / 4; ++k) {
                         const ulonglong2 bq = pB[k];
                         ulonglong2 cq = {0ull, 0ull};
-                        if (!CARRY) cq = pC[k];
+                        if (!CARRY) cq = pB[NP / 4 + k];
                         const F2 b2[2] = {{bq.x}, {bq.y}}, c2[2] = {{cq.x}, {cq.y}};
 #pragma unroll
-                        for (int i = 0; i < CPT; ++i)
-#pragma unroll
-                            for (int m = 0; m < 2; ++m) {
-                                float e0, e1;
-                                f2_split(f2_mul(d2[i], A2[i][2 * k + m]), e0, e1);
-                                const F2 decay = f2(exp2_fast(e0), exp2_fast(e1));
-                                F2& hh = h[i][2 * k + m];
-                                hh = f2_fma(decay, hh, f2_mul(du2[i], b2[m]));
-                                if (!CARRY) acc[i] = f2_fma(hh, c2[m], acc[i]);
-                            }
-                    }
-                    if (!CARRY) {
-#pragma unroll
-                        for (int i = 0; i < CPT; ++i) {
-                            float v0, v1;
-                            f2_split(acc[i], v0, v1);
-                            float v = v0 + v1;
-#pragma unroll
-                            for (int m = 1; m < LPC; m *= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
-                            v = fmaf(skip[i], u[i], v);
-                            if (zp) v *= silu(zv[j][i]);
-                            if (live[i] && (lane % LPC) == (uint32_t)(i % LPC))
-                                yp[(int64_t)(t + i0 + j) * a.y_stride + ch[i]] = from_f32<T>(v);
+                        for (int m = 0; m < 2; ++m) {
+                            float e0, e1;
+                            f2_split(f2_mul(d2, A2[2 * k + m]), e0, e1);
+                            const F2 decay = f2(exp2_fast(e0), exp2_fast(e1));
+                            F2& hh = h[2 * k + m];
+                            hh = f2_fma(decay, hh, f2_mul(du2, b2[m]));
+                            if (!CARRY) acc = f2_fma(hh, c2[m], acc);
                         }
                     }
+                    if (!CARRY) {
+                        float v0, v1;
+                        f2_split(acc, v0, v1);
+                        float v = v0 + v1;
+#pragma unroll
+                        for (int m = 1; m < LPC; m *= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
+                        v = fmaf(skip, u, v);
+                        if (a.z) v *= silu(zv[j]);
+                        if (live && n0 == 0u) py[j * a.y_stride] = from_f32<T>(v);
+                    }
                 }
+                py += U * a.y_stride;
             }
+            // (a tile that is not a whole number of groups is the job's last one)
             t += n_tok;
+            left -= n_tok;
+            buf ^= 1u;
         }
         if (!CARRY && ends && slot >= 0 && a.state) store_h(a.state + slot * (int64_t)DN);
     }
     if (CARRY) {
         store_h(a.seg_h + (uint64_t)seg * DN);
-#pragma unroll
-        for (int i = 0; i < CPT; ++i)
-            if (live[i] && n0 == 0u) a.seg_sdt[(uint64_t)seg * a.D + ch[i]] = sdt[i];
+        if (live && n0 == 0u) a.seg_sdt[(uint64_t)seg * a.D + ch] = sdt;
     }
 }
 
@@ -409,14 +419,17 @@ __global__ void __launch_bounds__(256) ssm_history_kernel(const SsmArgs a) {
     }
 }
 
-constexpr int SSM_STEP_THREADS = 256;
+constexpr uint32_t SSM_STEP_THREADS = 256;
 
-// Single tokens: a cluster of CTAs per job, 4 states of one channel per thread.  The state is read and written once;
-// every CTA convolves the job's B and C for itself, so the kept rows of B and C are replaced by the first CTA only
-// after the cluster has read them.
+// Single tokens.  A CTA takes 256 channels of a job at a time: while their states are on the way (four 16-byte pieces
+// a thread), each thread works out convolution, time step and gate of one channel; then the states are advanced,
+// written back, and summed against C over the lanes of a channel.  The CTAs of a job form a cluster: each convolves
+// the job's B and C for itself, so the kept rows of B and C are replaced only when the whole cluster has read them.
 template <typename T>
-__global__ void __launch_bounds__(SSM_STEP_THREADS) ssm_step_kernel(const SsmArgs a, uint32_t lanes, uint32_t vec) {
+__global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const SsmArgs a, uint32_t lanes, uint32_t vec) {
     extern __shared__ __align__(16) float s_bc[];           // B of all groups, then C, each padded to 4 * lanes
+    __shared__ float s_dt[SSM_STEP_THREADS], s_du[SSM_STEP_THREADS], s_y[SSM_STEP_THREADS];
+    constexpr int U = 4;
     dep_wait();
     uint32_t rank, n_rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -424,97 +437,126 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS) ssm_step_kernel(const SsmArg
     const uint32_t s = blockIdx.x / n_rank, tid = threadIdx.x, NP = 4u * lanes;
     const int64_t slot = slot_of(a, s);
     const T* row = static_cast<const T*>(a.xbc) + (int64_t)s * a.xbc_stride;
-    T* hist = a.W > 1u && a.history && slot >= 0 ? static_cast<T*>(a.history) + slot * (int64_t)(a.W - 1u) * a.rows : nullptr;
+    const uint32_t H = a.W > 1u ? a.W - 1u : 0u;
+    T* hist = H && a.history && slot >= 0 ? static_cast<T*>(a.history) + slot * (int64_t)H * a.rows : nullptr;
+    float* state = slot >= 0 && a.state ? a.state + slot * (int64_t)a.D * a.N : nullptr;
     auto convolve = [&](uint32_t col, float v, float (&past)[3]) {
-        if (a.W == 0u) return v;
-        float acc = fmaf(a.conv_w[(uint64_t)col * a.W + a.W - 1u], v, a.conv_b ? a.conv_b[col] : 0.0f);
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (k < (int)a.W - 1) {
-                past[k] = hist ? to_f32(hist[(uint64_t)k * a.rows + col]) : 0.0f;
-                acc = fmaf(a.conv_w[(uint64_t)col * a.W + k], past[k], acc);
-            }
+        for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H && hist ? to_f32(hist[(uint64_t)k * a.rows + col]) : 0.0f;
+        if (a.W == 0u) return v;
+        const float* w = a.conv_w + (uint64_t)col * a.W;
+        float acc = fmaf(w[H], v, a.conv_b ? a.conv_b[col] : 0.0f);
+#pragma unroll
+        for (uint32_t k = 0; k < 3u; ++k)
+            if (k < H) acc = fmaf(w[k], past[k], acc);
         return silu(acc);
     };
     auto shift = [&](uint32_t col, float v, const float (&past)[3]) {
-        if (!hist) return;
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (k < (int)a.W - 1)
-                hist[(uint64_t)k * a.rows + col] = from_f32<T>(k + 1 < (int)a.W - 1 ? past[k + 1 < 3 ? k + 1 : 2] : v);
+        for (uint32_t k = 0; k < 3u; ++k)
+            if (k < H && hist) hist[(uint64_t)k * a.rows + col] = from_f32<T>(k + 1u < H ? past[k < 2u ? k + 1u : 2u] : v);
     };
-    for (uint32_t i = tid; i < 2u * a.G * NP; i += SSM_STEP_THREADS) {
-        const uint32_t n = i % NP, which = i / NP;          // which: B of group 0 .. G - 1, then C
-        float v = 0.0f, past[3] = {0.0f, 0.0f, 0.0f};
-        if (n < a.N) {
-            const uint32_t col = a.D + which * a.N + n;
-            v = convolve(col, to_f32(row[col]), past);
-        }
-        s_bc[i] = v;
-    }
-    __syncthreads();
-    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
 
-    const uint32_t per = SSM_STEP_THREADS / lanes, sub = tid % lanes, Dg = a.D / a.G;
-    const uint32_t stride = per * n_rank;
-    for (uint32_t d = rank * per + tid / lanes; d < (a.D + stride - 1u) / stride * stride; d += stride) {
-        const bool live = d < a.D;
-        const uint32_t c = live ? d : 0u, n = sub * 4u;
-        float hv[4], av[4];
-        float* hp = slot >= 0 && a.state ? a.state + (slot * (int64_t)a.D + c) * a.N + n : nullptr;
-        const float* ap = a.A + (uint64_t)c * a.N + n;
-        if (vec) {
-            const float4 q = hp && n < a.N ? *reinterpret_cast<const float4*>(hp) : make_float4(0.f, 0.f, 0.f, 0.f);
-            const float4 p = n < a.N ? *reinterpret_cast<const float4*>(ap) : make_float4(0.f, 0.f, 0.f, 0.f);
-            hv[0] = q.x; hv[1] = q.y; hv[2] = q.z; hv[3] = q.w;
-            av[0] = p.x; av[1] = p.y; av[2] = p.z; av[3] = p.w;
-        } else {
+    const uint32_t sub = tid % lanes, n = sub * 4u, per = SSM_STEP_THREADS / lanes, Dg = a.D / a.G;
+    bool first = true;
+    for (uint32_t base = rank * SSM_STEP_THREADS; base < a.D; base += n_rank * SSM_STEP_THREADS) {
+        float4 hv[U], av[U];
+        auto fetch = [&](uint32_t p0) {                     // passes p0 .. p0 + 3 over the 256 channels
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                hv[k] = hp && n + k < a.N ? hp[k] : 0.0f;
-                av[k] = n + k < a.N ? ap[k] : 0.0f;
-            }
-        }
-        const float xv = to_f32(row[c]);
-        float past[3] = {0.0f, 0.0f, 0.0f};
-        const float u = convolve(c, xv, past);
-        const float dt = softplus(to_f32(static_cast<const T*>(a.dt)[(int64_t)s * a.dt_stride + c]) + (a.dt_bias ? a.dt_bias[c] : 0.0f));
-        const float* bq = s_bc + (c / Dg) * NP + n;
-        const float* cq = bq + a.G * NP;
-        float acc = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            hv[k] = fmaf(exp2_fast(dt * (av[k] * 1.44269504f)), hv[k], dt * u * bq[k]);
-            acc = fmaf(hv[k], cq[k], acc);
-        }
-        for (uint32_t m = 1; m < lanes; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
-        __syncwarp();                                       // all lanes have read the kept rows of their channel
-        if (live) {
-            if (hp) {
+            for (int j = 0; j < U; ++j) {
+                const uint32_t d = base + (p0 + j) * per + tid / lanes;
+                hv[j] = av[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (p0 + j >= lanes || d >= a.D) continue;
+                const uint64_t at = (uint64_t)d * a.N + n;
                 if (vec) {
-                    if (n < a.N) *reinterpret_cast<float4*>(hp) = make_float4(hv[0], hv[1], hv[2], hv[3]);
+                    if (n < a.N) {
+                        if (state) hv[j] = *reinterpret_cast<const float4*>(state + at);
+                        av[j] = *reinterpret_cast<const float4*>(a.A + at);
+                    }
                 } else {
+                    float* hq = &hv[j].x;
+                    float* aq = &av[j].x;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (n + k < a.N) hp[k] = hv[k];
+                    for (uint32_t k = 0; k < 4u; ++k)
+                        if (n + k < a.N) {
+                            if (state) hq[k] = state[at + k];
+                            aq[k] = a.A[at + k];
+                        }
                 }
             }
-            if (sub == 0u) {
-                float v = fmaf(a.skip ? a.skip[c] : 0.0f, u, acc);
-                if (a.z) v *= silu(to_f32(static_cast<const T*>(a.z)[(int64_t)s * a.z_stride + c]));
-                static_cast<T*>(a.y)[(int64_t)s * a.y_stride + c] = from_f32<T>(v);
-                shift(c, xv, past);
+        };
+        fetch(0);
+        const uint32_t c = base + tid;
+        float u = 0.0f, gate = 1.0f, skip = 0.0f;
+        if (c < a.D) {
+            const float xv = to_f32(row[c]);
+            float past[3];
+            u = convolve(c, xv, past);
+            shift(c, xv, past);
+            const float dt = softplus(to_f32(static_cast<const T*>(a.dt)[(int64_t)s * a.dt_stride + c]) + (a.dt_bias ? a.dt_bias[c] : 0.0f));
+            s_dt[tid] = dt;
+            s_du[tid] = dt * u;
+            if (a.z) gate = silu(to_f32(static_cast<const T*>(a.z)[(int64_t)s * a.z_stride + c]));
+            if (a.skip) skip = a.skip[c];
+        }
+        if (first)
+            for (uint32_t i = tid; i < 2u * a.G * NP; i += SSM_STEP_THREADS) {
+                const uint32_t m = i % NP, which = i / NP;  // which: B of group 0 .. G - 1, then C
+                float v = 0.0f, past[3];
+                if (m < a.N) {
+                    const uint32_t col = a.D + which * a.N + m;
+                    v = convolve(col, to_f32(row[col]), past);
+                }
+                s_bc[i] = v;
+            }
+        __syncthreads();
+        if (first) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        first = false;
+        for (uint32_t p0 = 0; p0 < lanes; p0 += U) {
+            if (p0) fetch(p0);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                if (p0 + j >= lanes) break;
+                const uint32_t local = (p0 + j) * per + tid / lanes, d = base + local;
+                const bool live = d < a.D;
+                const float dt = live ? s_dt[local] : 0.0f, du = live ? s_du[local] : 0.0f;
+                const float* bq = s_bc + (live ? d / Dg : 0u) * NP + n;
+                const float4 B = *reinterpret_cast<const float4*>(bq), C = *reinterpret_cast<const float4*>(bq + a.G * NP);
+                const float dl = dt * LOG2E;
+                hv[j].x = fmaf(exp2_fast(dl * av[j].x), hv[j].x, du * B.x);
+                hv[j].y = fmaf(exp2_fast(dl * av[j].y), hv[j].y, du * B.y);
+                hv[j].z = fmaf(exp2_fast(dl * av[j].z), hv[j].z, du * B.z);
+                hv[j].w = fmaf(exp2_fast(dl * av[j].w), hv[j].w, du * B.w);
+                float acc = fmaf(hv[j].x, C.x, hv[j].y * C.y) + fmaf(hv[j].z, C.z, hv[j].w * C.w);
+                for (uint32_t m = 1; m < lanes; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
+                if (live) {
+                    if (sub == 0u) s_y[local] = acc;
+                    const uint64_t at = (uint64_t)d * a.N + n;
+                    if (!state) continue;
+                    if (vec) {
+                        if (n < a.N) *reinterpret_cast<float4*>(state + at) = hv[j];
+                    } else {
+                        const float* hq = &hv[j].x;
+#pragma unroll
+                        for (uint32_t k = 0; k < 4u; ++k)
+                            if (n + k < a.N) state[at + k] = hq[k];
+                    }
+                }
             }
         }
+        __syncthreads();
+        if (c < a.D)
+            static_cast<T*>(a.y)[(int64_t)s * a.y_stride + c] = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
+        // (s_y is next written behind the next round's barrier, s_dt and s_du are not read any more)
     }
+    if (first) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");   // a CTA without channels
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (rank == 0u && hist)
         for (uint32_t i = tid; i < 2u * a.G * a.N; i += SSM_STEP_THREADS) {
             const uint32_t col = a.D + i;
-            float past[3] = {0.0f, 0.0f, 0.0f};
+            float past[3];
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
-                if (k < (int)a.W - 1) past[k] = to_f32(hist[(uint64_t)k * a.rows + col]);
+            for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H ? to_f32(hist[(uint64_t)k * a.rows + col]) : 0.0f;
             shift(col, to_f32(row[col]), past);
         }
 }

@@ -9,7 +9,6 @@
 namespace sja {
 
 constexpr uint32_t TOK_MAX_TOP = 32;
-constexpr float LN2 = 0.693147182f, LOG2E = 1.44269504f;
 
 struct TokenArgs {
     const void* logits;
