@@ -1516,6 +1516,9 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
 #ifndef SSM_WARPS_PER_SM
 #define SSM_WARPS_PER_SM 16u
 #endif
+#ifndef SSM_SNAP
+#define SSM_SNAP 2u
+#endif
 template <typename T>
 sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
     if (a.T > 0) {
@@ -1533,7 +1536,7 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         n_seg = std::min<uint64_t>(n_seg, 65535u);
         a.seg_len = (a.T + n_seg - 1u) / n_seg;
         a.n_seg = (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
-        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len / 2u, 0x7FFFFFFFu);
+        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len / SSM_SNAP, 0x7FFFFFFFu);
         if (a.n_seg > 1u) {
             const size_t DN = (size_t)a.D * a.N, n = a.n_seg;
             const size_t h = n * DN * 4u, f = a.resume && a.state ? h : 0u, s = n * a.D * 4u;
@@ -1576,6 +1579,45 @@ sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
     cfg.numAttrs = 2;
     CU(cudaLaunchKernelEx(&cfg, ssm_step_kernel<T>, a, lanes, vec));
     return SJA_OK;
+}
+
+template <typename T, int J>
+void launch_token_row(sja_ctx* c, const TokenArgs& a) {
+    launch_dep(token_row_kernel<T, J>, dim3((uint32_t)((a.R + TOK_ROW_WARPS - 1u) / TOK_ROW_WARPS)), TOK_ROW_WARPS * 32u, 0,
+               c->stream, a);
+}
+
+template <typename T, int THREADS>
+sja_status launch_token_stats(sja_ctx* c, const TokenArgs& a, uint32_t ctas) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((uint32_t)a.R * ctas);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = c->stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = ctas; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = ctas > 1u ? 2u : 1u;
+    CU(cudaLaunchKernelEx(&cfg, token_stats_kernel<T, THREADS>, a));
+    return SJA_OK;
+}
+
+template <typename T>
+sja_status run_token_stats(sja_ctx* c, const TokenArgs& a) {
+    constexpr uint32_t n = RowView<T>::n;
+    // a row of up to 8 vectors a lane (and one more that a misaligned row may take) stays in a warp's registers
+    const uint32_t vecs = (a.V + n - 1u) / n + ((uintptr_t)a.logits % 16u || (a.row_stride * sizeof(T)) % 16u ? 1u : 0u);
+    if (vecs <= 32u) { launch_token_row<T, 1>(c, a); return SJA_OK; }
+    if (vecs <= 64u) { launch_token_row<T, 2>(c, a); return SJA_OK; }
+    if (vecs <= 128u) { launch_token_row<T, 4>(c, a); return SJA_OK; }
+    if (vecs <= 256u) { launch_token_row<T, 8>(c, a); return SJA_OK; }
+    // few rows: up to eight CTAs share one, as long as each thread has a vector
+    uint32_t ctas = 1u;
+    while (ctas < 8u && a.R * ctas * 2u <= (uint64_t)c->n_sm && vecs > ctas * 256u) ctas *= 2u;
+    if (vecs / ctas <= 1024u) return launch_token_stats<T, 128>(c, a, ctas);
+    return launch_token_stats<T, 256>(c, a, ctas);
 }
 
 }  // namespace
@@ -1634,10 +1676,9 @@ sja_status sja_token_stats(sja_ctx* c, const sja_token_rows* m) {
     a.tokens = m->tokens; a.logp = m->logp; a.entropy = m->entropy; a.top_logp = m->top_logp; a.top_ids = m->top_ids;
     DeviceGuard guard(c->device);
     if (!guard.ok) return cuda_fail(c, cudaErrorInvalidDevice, "cudaSetDevice");
-    const dim3 grid((uint32_t)a.R);
-    if (m->dtype == SJA_F32) launch_dep(token_stats_kernel<float>, grid, TOK_THREADS, 0, c->stream, a);
-    else if (m->dtype == SJA_F16) launch_dep(token_stats_kernel<__half>, grid, TOK_THREADS, 0, c->stream, a);
-    else launch_dep(token_stats_kernel<__nv_bfloat16>, grid, TOK_THREADS, 0, c->stream, a);
+    if (m->dtype == SJA_F32) TRY(run_token_stats<float>(c, a));
+    else if (m->dtype == SJA_F16) TRY(run_token_stats<__half>(c, a));
+    else TRY(run_token_stats<__nv_bfloat16>(c, a));
     CU(cudaGetLastError());
     return SJA_OK;
 }

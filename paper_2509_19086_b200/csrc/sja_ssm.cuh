@@ -87,6 +87,11 @@ __device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
 __device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
     F2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
@@ -175,7 +180,7 @@ struct Conv {
 
 constexpr uint32_t SSM_THREADS = 256;    // most threads of a prompt CTA
 // Tokens whose B and C one CTA keeps at a time: a thread convolves a stretch of 8 tokens of one column (2 NP of them).
-__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np <= 32u ? 32u : 1024u / np; }
+__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return 1024u / np; }
 
 // Prompts.  A thread owns one channel and K of its states (LPC lanes share a channel), walks its segment of the token
 // axis and keeps the states in registers.  B and C of a tile of tokens are convolved once per CTA into shared memory,

@@ -49,29 +49,12 @@ __device__ __forceinline__ Stat stat_join(const Stat& a, const Stat& b, float c)
     return r;
 }
 
-template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
-
-// The elements of one 16-byte vector of the row (or fewer at its end), as 32-bit values.
-template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, bool aligned, uint32_t count, float (&v)[Vec<T>::n]) {
-    constexpr int n = Vec<T>::n;
-    if (aligned && count >= (uint32_t)n) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p);
-        const T* e = reinterpret_cast<const T*>(&q);
-#pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = to_f32(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = (uint32_t)i < count ? to_f32(p[i]) : -INFINITY;
-    }
-}
-
 // Row log probabilities from the joined sums.
 struct RowStat {
     float m, log_s, entropy;
-    bool empty;
+    __device__ __forceinline__ RowStat() {}
     __device__ __forceinline__ explicit RowStat(const Stat& t) {
-        empty = t.m == -INFINITY && t.s == 0.0f;
+        const bool empty = t.m == -INFINITY && t.s == 0.0f;      // nothing but -inf
         m = empty ? 0.0f : t.m;
         log_s = empty ? 0.0f : __log2f(t.s);
         entropy = empty ? 0.0f : LN2 * (log_s - t.w / t.s);
@@ -82,135 +65,435 @@ struct RowStat {
     }
 };
 
-constexpr int TOK_THREADS = 256, TOK_CAND = 2048;
-
-// One CTA per row, any vocabulary.  The alternatives: every thread knows its largest element; the r-th largest of
-// each warp's, r * warps >= top, bound the answer from below, so a second look at the row (which the cache still
-// holds) keeps a few dozen candidates, ranked by counting.  Rows on which the bound fails to thin the candidates out
-// take `top` rounds of a maximum instead.
+// A row seen as 16-byte vectors on the addresses where those start: vector v covers the elements v n - skew ..
+// v n - skew + n - 1, of which the first and the last vector may hold fewer of the row.
 template <typename T>
-__global__ void __launch_bounds__(TOK_THREADS) token_stats_kernel(const TokenArgs a) {
-    constexpr int n = Vec<T>::n, WARPS = TOK_THREADS / 32;
-    __shared__ Stat s_stat[WARPS];
-    __shared__ uint64_t s_bound[WARPS], s_cand[TOK_CAND], s_max[WARPS];
-    __shared__ uint32_t s_count;
-    dep_wait();
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
-    const uint64_t r = blockIdx.x;
-    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
-    const bool aligned = (reinterpret_cast<uintptr_t>(row) & 15u) == 0u;
-    if (tid == 0u) s_count = 0u;
+struct RowView {
+    static constexpr int n = 16 / sizeof(T);
+    const T* base;            // 16-byte aligned, `skew` elements before the row
+    uint32_t skew, V, n_vec;
+    __device__ __forceinline__ RowView(const T* row, uint32_t vocab) : V(vocab) {
+        skew = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T);
+        base = row - skew;
+        n_vec = (V + skew + n - 1u) / n;
+    }
+    // elements of vector v that are not the row's come back as -inf
+    __device__ __forceinline__ uint4 load(uint32_t v) const {
+        const int64_t first = (int64_t)v * n - skew;
+        if (first >= 0 && first + n <= (int64_t)V) return __ldg(reinterpret_cast<const uint4*>(base) + v);
+        uint4 q;
+        T* e = reinterpret_cast<T*>(&q);
+#pragma unroll
+        for (int j = 0; j < n; ++j)
+            e[j] = first + j >= 0 && first + j < (int64_t)V ? base[(int64_t)v * n + j] : from_f32<T>(-INFINITY);
+        return q;
+    }
+    __device__ __forceinline__ bool has(uint32_t v, int j) const {
+        const int64_t i = (int64_t)v * n - skew + j;
+        return i >= 0 && i < (int64_t)V;
+    }
+    __device__ __forceinline__ uint32_t index(uint32_t v, int j) const { return v * n - skew + j; }
+};
 
-    Stat st = {-INFINITY, 0.0f, 0.0f};
+__device__ __forceinline__ float max_of(const uint4& q, float) {
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+}
+__device__ __forceinline__ float max_of(const uint4& q, __half) {
+    const __half2* p = reinterpret_cast<const __half2*>(&q);
+    const __half2 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+    return __half2float(__hmax(__low2half(m), __high2half(m)));
+}
+__device__ __forceinline__ float max_of(const uint4& q, __nv_bfloat16) {
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&q);
+    const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
+    return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
+}
+template <typename T> __device__ __forceinline__ float elem(const uint4& q, int j) { return to_f32(reinterpret_cast<const T*>(&q)[j]); }
+
+__device__ __forceinline__ Stat stat_shuffle(Stat st, uint32_t m) {
+    Stat o;
+    o.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, m);
+    o.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, m);
+    o.w = __shfl_xor_sync(0xFFFFFFFFu, st.w, m);
+    return o;
+}
+
+// s and w of one vector relative to m (a finite number, or +inf / NaN where the row has such).
+template <typename T>
+__device__ __forceinline__ void add_vec(const uint4& q, float m, float c, float& s, float& w) {
+    const F2 nm = f2(-m, -m), cc = f2(c, c);
+    float s0 = 0.0f, s1 = 0.0f, w0 = 0.0f, w1 = 0.0f;
+#pragma unroll
+    for (int j = 0; j < RowView<T>::n; j += 2) {
+        float d0, d1;
+        f2_split(f2_mul(f2_add(f2(elem<T>(q, j), elem<T>(q, j + 1)), nm), cc), d0, d1);
+        const float e0 = exp2_fast(d0), e1 = exp2_fast(d1);
+        s0 += e0; s1 += e1;
+        w0 = fmaf(e0, fmaxf(d0, -200.0f), w0);          // 2^-200 is 0 here; -inf must not meet it
+        w1 = fmaf(e1, fmaxf(d1, -200.0f), w1);
+    }
+    s += s0 + s1;
+    w += w0 + w1;
+}
+
+// Log probability of the row's token and entropy, by one thread.
+template <typename T>
+__device__ __forceinline__ void put_row(const TokenArgs& a, uint64_t r, const T* row, const RowStat& rs) {
+    if (a.entropy) a.entropy[r] = rs.entropy;
+    if (a.logp) {
+        const int64_t t = a.tokens[r];
+        a.logp[r] = t < 0 ? 0.0f : t >= (int64_t)a.V ? __uint_as_float(0x7FC00000u) : rs.logp(to_f32(row[t]), a.scale);
+    }
+}
+// Alternative k of the row by its key; key 0: there is none.
+__device__ __forceinline__ void put_top(const TokenArgs& a, uint64_t r, uint32_t k, uint64_t key, const RowStat& rs) {
+    if (a.top_ids) a.top_ids[r * a.top + k] = key ? (int32_t)~(uint32_t)key : -1;
+    if (a.top_logp) a.top_logp[r * a.top + k] = key ? rs.logp(key_value((uint32_t)(key >> 32)), a.scale) : -INFINITY;
+}
+
+// Descending order of the warp's 32 values: lane i ends with the i-th largest.
+__device__ __forceinline__ float warp_sort_desc(float v) {
+    const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll
+    for (uint32_t k = 2; k <= 32u; k *= 2)
+#pragma unroll
+        for (uint32_t j = k / 2; j > 0; j /= 2) {
+            const float o = __shfl_xor_sync(0xFFFFFFFFu, v, j);
+            const bool keep_max = ((lane & k) == 0u) == ((lane & j) == 0u);
+            v = keep_max ? fmaxf(v, o) : fminf(v, o);
+        }
+    return v;
+}
+
+constexpr uint32_t TOK_ROW_WARPS = 8, TOK_ROW_CAND = 128;
+
+// Short rows: a warp per row, the row in registers (J vectors a lane).  The alternatives: the k-th largest of the 32
+// lanes' largest elements bounds the answer from below; what exceeds it, and the first k that equal it (in order of
+// index), are all that can be among the k largest.  They are ranked by counting.  Rows that put too many elements
+// into the same lanes take k rounds of a maximum.
+template <typename T, int J>
+__global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const TokenArgs a) {
+    constexpr int n = RowView<T>::n;
+    __shared__ __align__(16) uint64_t s_key[TOK_ROW_WARPS][TOK_ROW_CAND];
+    dep_wait();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint64_t r = (uint64_t)blockIdx.x * TOK_ROW_WARPS + warp;
+    if (r >= a.R) return;
+    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
+    const RowView<T> rv(row, a.V);
+    uint4 q[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const uint32_t v = lane + 32u * j;
+        if (v < rv.n_vec) {
+            q[j] = rv.load(v);
+        } else {
+            T* e = reinterpret_cast<T*>(&q[j]);
+#pragma unroll
+            for (int i = 0; i < n; ++i) e[i] = from_f32<T>(-INFINITY);
+        }
+    }
     float best = -INFINITY;
-    uint64_t key = 0ull;
-    for (uint32_t i = tid * n; i < a.V; i += TOK_THREADS * n) {
-        float v[n];
-        const uint32_t count = min(a.V - i, (uint32_t)n);
-        load_vec(row + i, aligned, count, v);
-        float vm = v[0];
 #pragma unroll
-        for (int j = 1; j < n; ++j) vm = fmaxf(vm, v[j]);
-        if (key == 0ull || vm > best) {
-            uint64_t k = 0ull;
+    for (int j = 0; j < J; ++j) best = fmaxf(best, max_of(q[j], T()));
+    Stat st = {best, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < n; ++j)
-                if ((uint32_t)j < count) k = max(k, order_key(v[j], i + j));
-            if (k > key) key = k;
-            if (vm > best) {
-                best = vm;
-                const float d = st.m == -INFINITY ? 0.0f : (st.m - best) * a.c, f = exp2_fast(d);
-                st.w = f * fmaf(st.s, fmaxf(d, -200.0f), st.w);
-                st.s *= f;
-                st.m = best;
-            }
-        }
-        const float m = st.m == -INFINITY ? 0.0f : st.m;
+    for (uint32_t m = 16; m; m /= 2) st.m = fmaxf(st.m, __shfl_xor_sync(0xFFFFFFFFu, st.m, m));
+    const float m0 = st.m == -INFINITY ? 0.0f : st.m;
 #pragma unroll
-        for (int j = 0; j < n; ++j) {
-            const float d = (v[j] - m) * a.c, e = exp2_fast(d);
-            st.s += e;
-            st.w = fmaf(e, fmaxf(d, -200.0f), st.w);
-        }
+    for (int j = 0; j < J; ++j) add_vec<T>(q[j], m0, a.c, st.s, st.w);
+#pragma unroll
+    for (uint32_t m = 16; m; m /= 2) {
+        st.s += __shfl_xor_sync(0xFFFFFFFFu, st.s, m);
+        st.w += __shfl_xor_sync(0xFFFFFFFFu, st.w, m);
     }
-    // a thread that has seen NaN only has best = -inf and a NaN sum: the sums carry it from here
-#pragma unroll
-    for (int m = 16; m; m >>= 1) {
-        Stat o;
-        o.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, m);
-        o.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, m);
-        o.w = __shfl_xor_sync(0xFFFFFFFFu, st.w, m);
-        st = stat_join(st, o, a.c);
-    }
-    if (lane == 0u) s_stat[warp] = st;
-    const uint32_t top = min(a.top, a.V);
-    if (top) {
-        uint64_t left = key, bound = 0ull;
-        for (uint32_t k = 0; k < (top + WARPS - 1u) / WARPS; ++k) {
-            bound = warp_max_u64(left);
-            if (left == bound) left = 0ull;
-        }
-        if (lane == 0u) s_bound[warp] = bound;
-    }
-    __syncthreads();
-    st = s_stat[0];
-    for (int w = 1; w < WARPS; ++w) st = stat_join(st, s_stat[w], a.c);
     const RowStat rs(st);
-    if (tid == 0u) {
-        if (a.entropy) a.entropy[r] = rs.entropy;
-        if (a.logp) {
-            const int64_t t = a.tokens[r];
-            a.logp[r] = t < 0 ? 0.0f : t >= (int64_t)a.V ? __uint_as_float(0x7FC00000u) : rs.logp(to_f32(row[t]), a.scale);
-        }
-    }
+    if (lane == 0u) put_row(a, r, row, rs);
     if (!a.top) return;
-    auto put = [&](uint32_t k, uint64_t q) {
-        const float v = key_value((uint32_t)(q >> 32));
-        if (a.top_ids) a.top_ids[r * a.top + k] = q ? (int32_t)~(uint32_t)q : -1;
-        if (a.top_logp) a.top_logp[r * a.top + k] = q ? rs.logp(v, a.scale) : -INFINITY;
-    };
-    for (uint32_t k = top + tid; k < a.top; k += TOK_THREADS) put(k, 0ull);
-    uint64_t bound = s_bound[0];
-    for (int w = 1; w < WARPS; ++w) bound = min(bound, s_bound[w]);
-    for (uint32_t i = tid * n; i < a.V; i += TOK_THREADS * n) {
-        float v[n];
-        const uint32_t count = min(a.V - i, (uint32_t)n);
-        load_vec(row + i, aligned, count, v);
+    const uint32_t top = min(a.top, a.V);
+    if (lane >= top && lane < a.top) put_top(a, r, lane, 0ull, rs);
+    const float tau = __shfl_sync(0xFFFFFFFFu, warp_sort_desc(best), top - 1u);
+
+    // one bit an element: above the bound, equal to it (-inf of a vector's foreign elements counts as equal to -inf,
+    // and is told apart below)
+    uint32_t n_above = 0, n_equal = 0;
 #pragma unroll
-        for (int j = 0; j < n; ++j) {
-            const uint64_t k = order_key(v[j], i + j);
-            if ((uint32_t)j < count && k >= bound) {
-                const uint32_t at = atomicAdd(&s_count, 1u);
-                if (at < TOK_CAND) s_cand[at] = k;
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float v = elem<T>(q[j], i);
+            n_above += v > tau;
+            n_equal += v == tau;
+        }
+    const uint32_t above_all = __reduce_add_sync(0xFFFFFFFFu, n_above);
+    uint64_t* key = s_key[warp];
+    uint32_t count = 0;
+    bool listed = above_all <= TOK_ROW_CAND - TOK_MAX_TOP;
+    if (listed) {
+        uint32_t before = n_above;                                   // exclusive sum over the lanes
+#pragma unroll
+        for (uint32_t m = 1; m < 32u; m *= 2) {
+            const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, before, m);
+            if (lane >= m) before += o;
+        }
+        before -= n_above;
+        if (n_above) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                if (!(max_of(q[j], T()) > tau)) continue;
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    const float v = elem<T>(q[j], i);
+                    if (v > tau) key[before++] = order_key(v, rv.index(lane + 32u * j, i));
+                }
             }
         }
+        // the bound itself, in order of index: vectors ascend with j, then with the lane
+        const bool plain = tau != -INFINITY;
+        uint32_t equal = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (equal >= top) break;
+            uint32_t mine = 0;
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                mine += elem<T>(q[j], i) == tau && (plain || rv.has(lane + 32u * j, i));
+            if (!__any_sync(0xFFFFFFFFu, mine)) continue;
+            uint32_t at = mine;
+#pragma unroll
+            for (uint32_t m = 1; m < 32u; m *= 2) {
+                const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, at, m);
+                if (lane >= m) at += o;
+            }
+            const uint32_t all = __shfl_sync(0xFFFFFFFFu, at, 31);
+            at += equal - mine;
+            if (mine) {
+#pragma unroll
+                for (int i = 0; i < n; ++i)
+                    if (elem<T>(q[j], i) == tau && (plain || rv.has(lane + 32u * j, i))) {
+                        if (at < top) key[above_all + at] = order_key(tau, rv.index(lane + 32u * j, i));
+                        ++at;
+                    }
+            }
+            equal += all;
+        }
+        count = above_all + min(equal, top);
+        listed = count >= top;                                       // NaN is neither above nor equal
     }
-    __syncthreads();
-    const uint32_t count = s_count;
-    if (count <= TOK_CAND) {
-        for (uint32_t i = tid; i < count; i += TOK_THREADS) {
-            const uint64_t k = s_cand[i];
+    __syncwarp();
+    if (listed) {
+        if (count & 1u) {                                            // pairs are read below
+            if (lane == 0u) key[count] = 0ull;
+            __syncwarp();
+        }
+        for (uint32_t i = lane; i < count; i += 32u) {
+            const uint64_t k = key[i];
             uint32_t rank = 0;
-            for (uint32_t j = 0; j < count && rank < top; ++j) rank += s_cand[j] > k;
-            if (rank < top) put(rank, k);
+            for (uint32_t o = 0; o < count; o += 2u) {
+                const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(key + o);
+                rank += (two.x > k) + (two.y > k);
+            }
+            if (rank < top) put_top(a, r, rank, k, rs);
         }
         return;
     }
     uint64_t below = ~0ull;
     for (uint32_t k = 0; k < top; ++k) {
         uint64_t most = 0ull;
-        for (uint32_t i = tid; i < a.V; i += TOK_THREADS) {
-            const uint64_t q = order_key(to_f32(row[i]), i);
-            if (q < below) most = max(most, q);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                if (rv.has(lane + 32u * j, i)) {
+                    const uint64_t x = order_key(elem<T>(q[j], i), rv.index(lane + 32u * j, i));
+                    if (x < below) most = max(most, x);
+                }
+        below = warp_max_u64(most);
+        if (lane == 0u) put_top(a, r, k, below, rs);
+    }
+}
+
+constexpr uint32_t TOK_CAND = 1024, TOK_GROUPS = 16;
+
+// Long rows: a CTA per row, or a cluster of CTAs, each with a slice of the row, where there are few rows.  One sweep,
+// four vectors at a time, with a running maximum per thread.  The alternatives: every thread knows its largest
+// element; the r-th largest of each warp's, r * warps >= top, bounds the slice's answer from below.  The sweep notes
+// the maximum of each stretch of a thread's vectors, so only stretches that reach the bound are read again.  The
+// candidates are ranked by counting, those of a cluster's slices once more in its first CTA.  Slices that keep too
+// many take `top` rounds of a maximum.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a) {
+    constexpr int n = RowView<T>::n, WARPS = THREADS / 32, U = 4;
+    __shared__ float s_group[TOK_GROUPS][THREADS];
+    __shared__ uint64_t s_cand[TOK_CAND], s_top[8][TOK_MAX_TOP], s_max[WARPS];
+    __shared__ Stat s_stat[WARPS], s_part[8];
+    __shared__ uint32_t s_count;
+    dep_wait();
+    uint32_t rank, n_rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_rank));
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
+    const uint64_t r = blockIdx.x / n_rank;
+    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
+    const RowView<T> rv(row, a.V);
+    const uint32_t per = (rv.n_vec + n_rank - 1u) / n_rank, lo = min(rank * per, rv.n_vec), hi = min(lo + per, rv.n_vec);
+    const uint32_t rounds = (per + THREADS * U - 1u) / (THREADS * U), stretch = (rounds + TOK_GROUPS - 1u) / TOK_GROUPS;
+    if (tid == 0u) s_count = 0u;
+
+    Stat st = {-INFINITY, 0.0f, 0.0f};
+    uint32_t best_at = lo + tid;                                     // vector with the thread's first largest element
+    float group = -INFINITY;
+    for (uint32_t k = 0; k < rounds; ++k) {
+        const uint32_t v0 = lo + k * (THREADS * U) + tid;
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t v = v0 + u * THREADS;
+            if (v < hi) q[u] = rv.load(v);
         }
-        most = warp_max_u64(most);
-        if (lane == 0u) s_max[warp] = most;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t v = v0 + u * THREADS;
+            if (v >= hi) break;
+            const float vm = max_of(q[u], T());
+            if (vm > st.m) {
+                const float d = st.m == -INFINITY ? 0.0f : (st.m - vm) * a.c, f = exp2_fast(d);
+                st.w = f * fmaf(st.s, fmaxf(d, -200.0f), st.w);
+                st.s *= f;
+                st.m = vm;
+                best_at = v;
+            }
+            group = fmaxf(group, vm);
+            add_vec<T>(q[u], st.m == -INFINITY ? 0.0f : st.m, a.c, st.s, st.w);
+        }
+        if ((k + 1u) % stretch == 0u || k + 1u == rounds) {
+            s_group[k / stretch][tid] = group;
+            group = -INFINITY;
+        }
+    }
+    // the thread's largest key: the first element of that value in the vector where it first appeared
+    uint64_t mine = 0ull;
+    if (a.top && best_at < hi) {
+        const uint4 q = rv.load(best_at);
+#pragma unroll
+        for (int j = 0; j < n; ++j)
+            if (rv.has(best_at, j)) mine = max(mine, order_key(elem<T>(q, j), rv.index(best_at, j)));
+    }
+    Stat all = st;
+#pragma unroll
+    for (uint32_t m = 16; m; m /= 2) all = stat_join(all, stat_shuffle(all, m), a.c);
+    if (lane == 0u) s_stat[warp] = all;
+    const uint32_t size = hi > lo ? (uint32_t)(min((int64_t)a.V, (int64_t)hi * n - rv.skew) - max((int64_t)0, (int64_t)lo * n - rv.skew)) : 0u;
+    const uint32_t top = min(a.top, size);                           // of this slice
+    if (a.top) {
+        uint64_t left = mine, bound = 0ull;
+        for (uint32_t k = 0; k < (a.top + WARPS - 1u) / WARPS; ++k) {
+            bound = warp_max_u64(left);
+            if (left == bound) left = 0ull;
+        }
+        if (lane == 0u) s_max[warp] = bound;
+    }
+    __syncthreads();
+    all = s_stat[0];
+    for (int w = 1; w < WARPS; ++w) all = stat_join(all, s_stat[w], a.c);
+    RowStat rs;
+    if (n_rank == 1u) {
+        rs = RowStat(all);
+        if (tid == 0u) put_row(a, r, row, rs);
+        if (!a.top) return;
+        for (uint32_t k = top + tid; k < a.top; k += THREADS) put_top(a, r, k, 0ull, rs);
+    }
+    auto put = [&](uint32_t k, uint64_t key) {
+        if (n_rank == 1u) put_top(a, r, k, key, rs);
+        else s_top[rank][k] = key;
+    };
+    if (a.top) {
+        uint64_t bound = s_max[0];
+        for (int w = 1; w < WARPS; ++w) bound = min(bound, s_max[w]);
+        const uint32_t bound_value = (uint32_t)(bound >> 32);
+        for (uint32_t k = 0; k < rounds; k += stretch) {
+            // (a thread that met nothing but NaN has a maximum of -inf, above NaN's own place in the order)
+            if (value_key(s_group[k / stretch][tid]) < bound_value) continue;
+            for (uint32_t v = lo + k * (THREADS * U) + tid, i = 0; i < stretch * U && v < hi; ++i, v += THREADS) {
+                const uint4 q = rv.load(v);
+                if (value_key(max_of(q, T())) < bound_value) continue;
+#pragma unroll
+                for (int j = 0; j < n; ++j) {
+                    const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
+                    if (key >= bound && rv.has(v, j)) {
+                        const uint32_t at = atomicAdd(&s_count, 1u);
+                        if (at < TOK_CAND) s_cand[at] = key;
+                    }
+                }
+            }
+        }
         __syncthreads();
-        most = s_max[0];
-        for (int w = 1; w < WARPS; ++w) most = max(most, s_max[w]);
-        if (tid == 0u) put(k, most);
-        below = most;
-        __syncthreads();
+        const uint32_t count = s_count;
+        if (count <= TOK_CAND) {
+            for (uint32_t i = tid; i < count; i += THREADS) {
+                const uint64_t k = s_cand[i];
+                uint32_t place = 0;
+                for (uint32_t j = 0; j < count && place < top; ++j) place += s_cand[j] > k;
+                if (place < top) put(place, k);
+            }
+        } else {
+            uint64_t below = ~0ull;
+            for (uint32_t k = 0; k < top; ++k) {
+                uint64_t most = 0ull;
+                for (uint32_t v = lo + tid; v < hi; v += THREADS) {
+                    const uint4 q = rv.load(v);
+#pragma unroll
+                    for (int j = 0; j < n; ++j) {
+                        const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
+                        if (key < below && rv.has(v, j)) most = max(most, key);
+                    }
+                }
+                __syncthreads();
+                most = warp_max_u64(most);
+                if (lane == 0u) s_max[warp] = most;
+                __syncthreads();
+                below = s_max[0];
+                for (int w = 1; w < WARPS; ++w) below = max(below, s_max[w]);
+                if (tid == 0u) put(k, below);
+            }
+        }
+    }
+    if (n_rank == 1u) return;
+
+    // the slices meet in the first CTA of the cluster
+    for (uint32_t k = top + tid; k < a.top; k += THREADS) s_top[rank][k] = 0ull;
+    __syncthreads();
+    auto remote = [&](const void* p) {
+        uint32_t local = (uint32_t)__cvta_generic_to_shared(p), there;
+        asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(local));
+        return there;
+    };
+    if (rank) {
+        if (tid < a.top) asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(remote(&s_top[rank][tid])), "l"(s_top[rank][tid]) : "memory");
+        if (tid == 0u) {
+            asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(remote(&s_part[rank].m)), "f"(all.m) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(remote(&s_part[rank].s)), "f"(all.s) : "memory");
+            asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(remote(&s_part[rank].w)), "f"(all.w) : "memory");
+        }
+    } else if (tid == 0u) {
+        s_part[0] = all;
+    }
+    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (rank) return;
+    all = s_part[0];
+    for (uint32_t w = 1; w < n_rank; ++w) all = stat_join(all, s_part[w], a.c);
+    rs = RowStat(all);
+    if (tid == 0u) put_row(a, r, row, rs);
+    const uint32_t want = min(a.top, a.V);
+    for (uint32_t k = want + tid; k < a.top; k += THREADS) put_top(a, r, k, 0ull, rs);
+    for (uint32_t i = tid; i < n_rank * a.top; i += THREADS) {
+        const uint64_t key = s_top[i / a.top][i % a.top];
+        if (!key) continue;
+        uint32_t place = 0;
+        for (uint32_t w = 0; w < n_rank; ++w)
+            for (uint32_t k = 0; k < a.top; ++k) place += s_top[w][k] > key;
+        if (place < want) put_top(a, r, place, key, rs);
     }
 }
 
