@@ -71,26 +71,25 @@ template <typename T>
 struct RowView {
     static constexpr int n = 16 / sizeof(T);
     const T* base;            // 16-byte aligned, `skew` elements before the row
-    uint32_t skew, V, n_vec;
+    uint32_t skew, V, n_vec, whole_at, whole;      // vectors whole_at .. whole_at + whole - 1 hold n elements of the row
     __device__ __forceinline__ RowView(const T* row, uint32_t vocab) : V(vocab) {
         skew = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T);
         base = row - skew;
         n_vec = (V + skew + n - 1u) / n;
+        whole_at = skew ? 1u : 0u;
+        whole = (V + skew) / n > whole_at ? (V + skew) / n - whole_at : 0u;
     }
     // elements of vector v that are not the row's come back as -inf
     __device__ __forceinline__ uint4 load(uint32_t v) const {
-        const int64_t first = (int64_t)v * n - skew;
-        if (first >= 0 && first + n <= (int64_t)V) return __ldg(reinterpret_cast<const uint4*>(base) + v);
+        if (v - whole_at < whole) return __ldg(reinterpret_cast<const uint4*>(base) + v);
         uint4 q;
         T* e = reinterpret_cast<T*>(&q);
 #pragma unroll
-        for (int j = 0; j < n; ++j)
-            e[j] = first + j >= 0 && first + j < (int64_t)V ? base[(int64_t)v * n + j] : from_f32<T>(-INFINITY);
+        for (int j = 0; j < n; ++j) e[j] = has(v, j) ? base[(int64_t)v * n + j] : from_f32<T>(-INFINITY);
         return q;
     }
     __device__ __forceinline__ bool has(uint32_t v, int j) const {
-        const int64_t i = (int64_t)v * n - skew + j;
-        return i >= 0 && i < (int64_t)V;
+        return index(v, j) < V;                       // (an element before the row wraps round)
     }
     __device__ __forceinline__ uint32_t index(uint32_t v, int j) const { return v * n - skew + j; }
 };
@@ -118,23 +117,67 @@ __device__ __forceinline__ Stat stat_shuffle(Stat st, uint32_t m) {
     return o;
 }
 
-// s and w of one vector relative to m (a finite number, or +inf / NaN where the row has such).
+// Sums of vectors relative to m (a finite number, or +inf / NaN where the row has such), two elements at a time.
 template <typename T>
-__device__ __forceinline__ void add_vec(const uint4& q, float m, float c, float& s, float& w) {
-    const F2 nm = f2(-m, -m), cc = f2(c, c);
-    float s0 = 0.0f, s1 = 0.0f, w0 = 0.0f, w1 = 0.0f;
+__device__ __forceinline__ void add_vec(const uint4& q, F2 minus_m, F2 c, F2& s, F2& w) {
 #pragma unroll
     for (int j = 0; j < RowView<T>::n; j += 2) {
         float d0, d1;
-        f2_split(f2_mul(f2_add(f2(elem<T>(q, j), elem<T>(q, j + 1)), nm), cc), d0, d1);
-        const float e0 = exp2_fast(d0), e1 = exp2_fast(d1);
-        s0 += e0; s1 += e1;
-        w0 = fmaf(e0, fmaxf(d0, -200.0f), w0);          // 2^-200 is 0 here; -inf must not meet it
-        w1 = fmaf(e1, fmaxf(d1, -200.0f), w1);
+        f2_split(f2_mul(f2_add(f2(elem<T>(q, j), elem<T>(q, j + 1)), minus_m), c), d0, d1);
+        const F2 e = f2(exp2_fast(d0), exp2_fast(d1));
+        s = f2_add(s, e);
+        w = f2_fma(e, f2(fmaxf(d0, -200.0f), fmaxf(d1, -200.0f)), w);    // 2^-200 is 0 here; -inf must not meet it
     }
-    s += s0 + s1;
-    w += w0 + w1;
 }
+__device__ __forceinline__ float f2_sum(F2 v) {
+    float a, b;
+    f2_split(v, a, b);
+    return a + b;
+}
+template <typename T> __device__ __forceinline__ uint4 empty_vec() {
+    uint4 q;
+    T* e = reinterpret_cast<T*>(&q);
+#pragma unroll
+    for (int j = 0; j < RowView<T>::n; ++j) e[j] = from_f32<T>(-INFINITY);
+    return q;
+}
+
+// Which of a lane's J vectors' elements are >= bound, as bits; bit_place says where a bit's element is.
+__device__ __forceinline__ uint32_t pair_ge(uint32_t q, float bound, __half) {
+    return __hge2_mask(*reinterpret_cast<const __half2*>(&q), __float2half2_rn(bound));
+}
+__device__ __forceinline__ uint32_t pair_ge(uint32_t q, float bound, __nv_bfloat16) {
+    return __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&q), __float2bfloat162_rn(bound));
+}
+template <typename T, int J> struct Bits {
+    static constexpr bool pairs = sizeof(T) == 2;
+    static constexpr int words = pairs && J > 4 ? J / 4 : 1;
+    uint32_t w[words];
+    __device__ __forceinline__ void set(const uint4 (&q)[J], float bound) {
+#pragma unroll
+        for (int i = 0; i < words; ++i) w[i] = 0u;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const uint32_t part[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (pairs) w[j / 4] |= pair_ge(part[i], bound, T()) & (0x00010001u << ((j % 4) * 4 + i));
+                else w[0] |= __uint_as_float(part[i]) >= bound ? 1u << (j * 4 + i) : 0u;
+            }
+        }
+    }
+    __device__ __forceinline__ uint32_t count() const {
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < words; ++i) n += __popc(w[i]);
+        return n;
+    }
+    // element offset, within the lane's vectors laid end to end, of bit b of word i
+    static __device__ __forceinline__ uint32_t place(int i, uint32_t b) {
+        if constexpr (pairs) return (uint32_t)i * 32u + (b & 15u) * 2u + (b >> 4);
+        else return b;
+    }
+};
 
 // Log probability of the row's token and entropy, by one thread.
 template <typename T>
@@ -167,9 +210,53 @@ __device__ __forceinline__ float warp_sort_desc(float v) {
 
 constexpr uint32_t TOK_ROW_WARPS = 8, TOK_ROW_CAND = 128;
 
+__device__ __forceinline__ uint32_t warp_sum_before(uint32_t v) {
+    const uint32_t lane = threadIdx.x & 31u;
+    uint32_t sum = v;
+#pragma unroll
+    for (uint32_t m = 1; m < 32u; m *= 2) {
+        const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, sum, m);
+        if (lane >= m) sum += o;
+    }
+    return sum - v;
+}
+
+// Rows in which too many elements reach the bound: those above it, and the first `top` that equal it in order of
+// index (vectors ascend with j, then with the lane).  False if even those above are too many, or NaN is needed.
+template <typename T, int J>
+__device__ __noinline__ bool token_row_ties(const uint4 (&q)[J], const RowView<T>& rv, float tau, uint32_t top, uint64_t* key, uint32_t& count) {
+    constexpr int n = RowView<T>::n;
+    const uint32_t lane = threadIdx.x & 31u;
+    uint32_t above = 0;
+    for (int j = 0; j < J; ++j)
+        for (int i = 0; i < n; ++i) above += elem<T>(q[j], i) > tau;
+    const uint32_t above_all = __reduce_add_sync(0xFFFFFFFFu, above);
+    if (above_all > TOK_ROW_CAND - TOK_MAX_TOP) return false;
+    uint32_t at = warp_sum_before(above), equal = 0;
+    for (int j = 0; j < J; ++j)
+        for (int i = 0; i < n; ++i) {
+            const float v = elem<T>(q[j], i);
+            if (v > tau) key[at++] = order_key(v, rv.index(lane + 32u * j, i));
+        }
+    for (int j = 0; j < J && equal < top; ++j) {
+        uint32_t mine = 0;
+        for (int i = 0; i < n; ++i) mine += elem<T>(q[j], i) == tau && rv.has(lane + 32u * j, i);
+        uint32_t to = equal + warp_sum_before(mine);
+        for (int i = 0; i < n; ++i)
+            if (elem<T>(q[j], i) == tau && rv.has(lane + 32u * j, i)) {
+                if (to < top) key[above_all + to] = order_key(tau, rv.index(lane + 32u * j, i));
+                ++to;
+            }
+        equal += __reduce_add_sync(0xFFFFFFFFu, mine);
+    }
+    count = above_all + min(equal, top);
+    if ((count & 1u) && lane == 0u) key[count] = 0ull;       // the list is read in pairs
+    return count >= top;
+}
+
 // Short rows: a warp per row, the row in registers (J vectors a lane).  The alternatives: the k-th largest of the 32
-// lanes' largest elements bounds the answer from below; what exceeds it, and the first k that equal it (in order of
-// index), are all that can be among the k largest.  They are ranked by counting.  Rows that put too many elements
+// lanes' largest elements bounds the answer from below.  What reaches it -- on rows with many ties: what exceeds it,
+// and the first k that equal it -- is listed in shared memory and ranked by counting.  Rows that put too many elements
 // into the same lanes take k rounds of a maximum.
 template <typename T, int J>
 __global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const TokenArgs a) {
@@ -183,16 +270,7 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const Tok
     const RowView<T> rv(row, a.V);
     uint4 q[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-        const uint32_t v = lane + 32u * j;
-        if (v < rv.n_vec) {
-            q[j] = rv.load(v);
-        } else {
-            T* e = reinterpret_cast<T*>(&q[j]);
-#pragma unroll
-            for (int i = 0; i < n; ++i) e[i] = from_f32<T>(-INFINITY);
-        }
-    }
+    for (int j = 0; j < J; ++j) q[j] = lane + 32u * j < rv.n_vec ? rv.load(lane + 32u * j) : empty_vec<T>();
     float best = -INFINITY;
 #pragma unroll
     for (int j = 0; j < J; ++j) best = fmaxf(best, max_of(q[j], T()));
@@ -200,8 +278,14 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const Tok
 #pragma unroll
     for (uint32_t m = 16; m; m /= 2) st.m = fmaxf(st.m, __shfl_xor_sync(0xFFFFFFFFu, st.m, m));
     const float m0 = st.m == -INFINITY ? 0.0f : st.m;
+    {
+        F2 ss = f2(0.0f, 0.0f), ww = ss;
+        const F2 nm = f2(-m0, -m0), cc = f2(a.c, a.c);
 #pragma unroll
-    for (int j = 0; j < J; ++j) add_vec<T>(q[j], m0, a.c, st.s, st.w);
+        for (int j = 0; j < J; ++j) add_vec<T>(q[j], nm, cc, ss, ww);
+        st.s = f2_sum(ss);
+        st.w = f2_sum(ww);
+    }
 #pragma unroll
     for (uint32_t m = 16; m; m /= 2) {
         st.s += __shfl_xor_sync(0xFFFFFFFFu, st.s, m);
@@ -214,80 +298,46 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const Tok
     if (lane >= top && lane < a.top) put_top(a, r, lane, 0ull, rs);
     const float tau = __shfl_sync(0xFFFFFFFFu, warp_sort_desc(best), top - 1u);
 
-    // one bit an element: above the bound, equal to it (-inf of a vector's foreign elements counts as equal to -inf,
-    // and is told apart below)
-    uint32_t n_above = 0, n_equal = 0;
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int i = 0; i < n; ++i) {
-            const float v = elem<T>(q[j], i);
-            n_above += v > tau;
-            n_equal += v == tau;
-        }
-    const uint32_t above_all = __reduce_add_sync(0xFFFFFFFFu, n_above);
     uint64_t* key = s_key[warp];
     uint32_t count = 0;
-    bool listed = above_all <= TOK_ROW_CAND - TOK_MAX_TOP;
+    Bits<T, J> bits;
+    bits.set(q, tau);
+    const uint32_t mine = bits.count();
+    const uint32_t all = __reduce_add_sync(0xFFFFFFFFu, mine);
+    bool listed = all < TOK_ROW_CAND;
     if (listed) {
-        uint32_t before = n_above;                                   // exclusive sum over the lanes
+        uint32_t* where = reinterpret_cast<uint32_t*>(key);
+        uint32_t at = warp_sum_before(mine);
 #pragma unroll
-        for (uint32_t m = 1; m < 32u; m *= 2) {
-            const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, before, m);
-            if (lane >= m) before += o;
-        }
-        before -= n_above;
-        if (n_above) {
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                if (!(max_of(q[j], T()) > tau)) continue;
-#pragma unroll
-                for (int i = 0; i < n; ++i) {
-                    const float v = elem<T>(q[j], i);
-                    if (v > tau) key[before++] = order_key(v, rv.index(lane + 32u * j, i));
-                }
+        for (int i = 0; i < bits.words; ++i)
+            for (uint32_t left = bits.w[i]; left; left &= left - 1u) {
+                const uint32_t p = bits.place(i, (uint32_t)__ffs((int)left) - 1u);
+                where[at++] = rv.index(lane + 32u * (p / n), (int)(p % n));
             }
+        __syncwarp();
+        uint64_t k[TOK_ROW_CAND / 32u];
+#pragma unroll
+        for (uint32_t i = 0; i < TOK_ROW_CAND / 32u; ++i) {
+            const uint32_t idx = i * 32u + lane < all ? where[i * 32u + lane] : a.V;
+            k[i] = idx < a.V ? order_key(to_f32(row[idx]), idx) : 0ull;      // a vector's foreign elements rank last
         }
-        // the bound itself, in order of index: vectors ascend with j, then with the lane
-        const bool plain = tau != -INFINITY;
-        uint32_t equal = 0;
+        count = all;
+        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (equal >= top) break;
-            uint32_t mine = 0;
+        for (uint32_t i = 0; i < TOK_ROW_CAND / 32u; ++i)
+            if (i * 32u <= all) key[i * 32u + lane] = k[i];                  // (and zeros behind the list)
+        uint32_t real = 0;
 #pragma unroll
-            for (int i = 0; i < n; ++i)
-                mine += elem<T>(q[j], i) == tau && (plain || rv.has(lane + 32u * j, i));
-            if (!__any_sync(0xFFFFFFFFu, mine)) continue;
-            uint32_t at = mine;
-#pragma unroll
-            for (uint32_t m = 1; m < 32u; m *= 2) {
-                const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, at, m);
-                if (lane >= m) at += o;
-            }
-            const uint32_t all = __shfl_sync(0xFFFFFFFFu, at, 31);
-            at += equal - mine;
-            if (mine) {
-#pragma unroll
-                for (int i = 0; i < n; ++i)
-                    if (elem<T>(q[j], i) == tau && (plain || rv.has(lane + 32u * j, i))) {
-                        if (at < top) key[above_all + at] = order_key(tau, rv.index(lane + 32u * j, i));
-                        ++at;
-                    }
-            }
-            equal += all;
-        }
-        count = above_all + min(equal, top);
-        listed = count >= top;                                       // NaN is neither above nor equal
+        for (uint32_t i = 0; i < TOK_ROW_CAND / 32u; ++i) real += k[i] != 0ull;
+        listed = __reduce_add_sync(0xFFFFFFFFu, real) >= top;                // NaN is not >= anything
+    } else {
+        listed = token_row_ties<T, J>(q, rv, tau, top, key, count);
     }
     __syncwarp();
     if (listed) {
-        if (count & 1u) {                                            // pairs are read below
-            if (lane == 0u) key[count] = 0ull;
-            __syncwarp();
-        }
         for (uint32_t i = lane; i < count; i += 32u) {
             const uint64_t k = key[i];
+            if (!k) continue;
             uint32_t rank = 0;
             for (uint32_t o = 0; o < count; o += 2u) {
                 const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(key + o);
@@ -342,35 +392,37 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
 
     Stat st = {-INFINITY, 0.0f, 0.0f};
     uint32_t best_at = lo + tid;                                     // vector with the thread's first largest element
+    F2 ss = f2(0.0f, 0.0f), ww = ss;
+    const F2 cc = f2(a.c, a.c);
     float group = -INFINITY;
     for (uint32_t k = 0; k < rounds; ++k) {
         const uint32_t v0 = lo + k * (THREADS * U) + tid;
         uint4 q[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t v = v0 + u * THREADS;
-            if (v < hi) q[u] = rv.load(v);
-        }
+        for (int u = 0; u < U; ++u) q[u] = v0 + u * THREADS < hi ? rv.load(v0 + u * THREADS) : empty_vec<T>();
+        float most = st.m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t v = v0 + u * THREADS;
-            if (v >= hi) break;
             const float vm = max_of(q[u], T());
-            if (vm > st.m) {
-                const float d = st.m == -INFINITY ? 0.0f : (st.m - vm) * a.c, f = exp2_fast(d);
-                st.w = f * fmaf(st.s, fmaxf(d, -200.0f), st.w);
-                st.s *= f;
-                st.m = vm;
-                best_at = v;
-            }
+            best_at = vm > most ? v0 + u * THREADS : best_at;
+            most = fmaxf(most, vm);
             group = fmaxf(group, vm);
-            add_vec<T>(q[u], st.m == -INFINITY ? 0.0f : st.m, a.c, st.s, st.w);
         }
+        // the sums so far move to the new maximum; without a branch, so that a warp stays together
+        const float m0 = most == -INFINITY ? 0.0f : most, d = st.m == -INFINITY ? 0.0f : (st.m - m0) * a.c, f = exp2_fast(d);
+        ww = f2_mul(f2(f, f), f2_fma(ss, f2(fmaxf(d, -200.0f), fmaxf(d, -200.0f)), ww));
+        ss = f2_mul(f2(f, f), ss);
+        st.m = most;
+        const F2 nm = f2(-m0, -m0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) add_vec<T>(q[u], nm, cc, ss, ww);
         if ((k + 1u) % stretch == 0u || k + 1u == rounds) {
             s_group[k / stretch][tid] = group;
             group = -INFINITY;
         }
     }
+    st.s = f2_sum(ss);
+    st.w = f2_sum(ww);
     // the thread's largest key: the first element of that value in the vector where it first appeared
     uint64_t mine = 0ull;
     if (a.top && best_at < hi) {
@@ -410,25 +462,39 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
     if (a.top) {
         uint64_t bound = s_max[0];
         for (int w = 1; w < WARPS; ++w) bound = min(bound, s_max[w]);
-        const uint32_t bound_value = (uint32_t)(bound >> 32);
-        for (uint32_t k = 0; k < rounds; k += stretch) {
-            // (a thread that met nothing but NaN has a maximum of -inf, above NaN's own place in the order)
-            if (value_key(s_group[k / stretch][tid]) < bound_value) continue;
-            for (uint32_t v = lo + k * (THREADS * U) + tid, i = 0; i < stretch * U && v < hi; ++i, v += THREADS) {
-                const uint4 q = rv.load(v);
-                if (value_key(max_of(q, T())) < bound_value) continue;
+        uint32_t count;
+        for (int attempt = 0;; ++attempt) {
+            const uint32_t bound_value = (uint32_t)(bound >> 32);
+            for (uint32_t k = 0; k < rounds; k += stretch) {
+                // (a thread that met nothing but NaN has a maximum of -inf, above NaN's own place in the order)
+                if (value_key(s_group[k / stretch][tid]) < bound_value) continue;
+                for (uint32_t v = lo + k * (THREADS * U) + tid, i = 0; i < stretch * U && v < hi; ++i, v += THREADS) {
+                    const uint4 q = rv.load(v);
+                    if (value_key(max_of(q, T())) < bound_value) continue;
 #pragma unroll
-                for (int j = 0; j < n; ++j) {
-                    const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
-                    if (key >= bound && rv.has(v, j)) {
-                        const uint32_t at = atomicAdd(&s_count, 1u);
-                        if (at < TOK_CAND) s_cand[at] = key;
+                    for (int j = 0; j < n; ++j) {
+                        const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
+                        if (key >= bound && rv.has(v, j)) {
+                            const uint32_t at = atomicAdd(&s_count, 1u);
+                            if (at < TOK_CAND) s_cand[at] = key;
+                        }
                     }
                 }
             }
+            __syncthreads();
+            count = s_count;
+            if (count <= TOK_CAND || attempt) break;
+            // many equal elements, or a warp with nothing large: the top-th largest of all threads' keys
+            __syncthreads();
+            s_cand[tid] = mine;
+            if (tid == 0u) { s_count = 0u; s_max[0] = 0ull; }
+            __syncthreads();
+            uint32_t place = 0;
+            for (uint32_t j = 0; j < THREADS; ++j) place += s_cand[j] > mine;
+            if (mine && place + 1u == min(a.top, (uint32_t)THREADS)) s_max[0] = mine;
+            __syncthreads();
+            bound = s_max[0];                              // (0: fewer threads than that have an element)
         }
-        __syncthreads();
-        const uint32_t count = s_count;
         if (count <= TOK_CAND) {
             for (uint32_t i = tid; i < count; i += THREADS) {
                 const uint64_t k = s_cand[i];
