@@ -222,29 +222,35 @@ __device__ __forceinline__ uint32_t warp_sum_before(uint32_t v) {
 }
 
 // Rows in which too many elements reach the bound: those above it, and the first `top` that equal it in order of
-// index (vectors ascend with j, then with the lane).  False if even those above are too many, or NaN is needed.
-template <typename T, int J>
-__device__ __noinline__ bool token_row_ties(const uint4 (&q)[J], const RowView<T>& rv, float tau, uint32_t top, uint64_t* key, uint32_t& count) {
+// index.  The row is read again (from the nearest cache).  False if even those above are too many, or NaN is needed.
+template <typename T>
+__device__ __noinline__ bool token_row_ties(const RowView<T>& rv, float tau, uint32_t top, uint64_t* key, uint32_t& count) {
     constexpr int n = RowView<T>::n;
     const uint32_t lane = threadIdx.x & 31u;
     uint32_t above = 0;
-    for (int j = 0; j < J; ++j)
-        for (int i = 0; i < n; ++i) above += elem<T>(q[j], i) > tau;
+    for (uint32_t v = lane; v < rv.n_vec; v += 32u) {
+        const uint4 q = rv.load(v);
+#pragma unroll
+        for (int i = 0; i < n; ++i) above += elem<T>(q, i) > tau;
+    }
     const uint32_t above_all = __reduce_add_sync(0xFFFFFFFFu, above);
     if (above_all > TOK_ROW_CAND - TOK_MAX_TOP) return false;
     uint32_t at = warp_sum_before(above), equal = 0;
-    for (int j = 0; j < J; ++j)
-        for (int i = 0; i < n; ++i) {
-            const float v = elem<T>(q[j], i);
-            if (v > tau) key[at++] = order_key(v, rv.index(lane + 32u * j, i));
-        }
-    for (int j = 0; j < J && equal < top; ++j) {
+    for (uint32_t v0 = 0; v0 < rv.n_vec; v0 += 32u) {
+        const uint32_t v = v0 + lane;
+        const uint4 q = v < rv.n_vec ? rv.load(v) : empty_vec<T>();
         uint32_t mine = 0;
-        for (int i = 0; i < n; ++i) mine += elem<T>(q[j], i) == tau && rv.has(lane + 32u * j, i);
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float x = elem<T>(q, i);
+            if (x > tau) key[at++] = order_key(x, rv.index(v, i));
+            mine += x == tau && rv.has(v, i);
+        }
         uint32_t to = equal + warp_sum_before(mine);
+#pragma unroll
         for (int i = 0; i < n; ++i)
-            if (elem<T>(q[j], i) == tau && rv.has(lane + 32u * j, i)) {
-                if (to < top) key[above_all + to] = order_key(tau, rv.index(lane + 32u * j, i));
+            if (elem<T>(q, i) == tau && rv.has(v, i)) {
+                if (to < top) key[above_all + to] = order_key(tau, rv.index(v, i));
                 ++to;
             }
         equal += __reduce_add_sync(0xFFFFFFFFu, mine);
@@ -254,14 +260,31 @@ __device__ __noinline__ bool token_row_ties(const uint4 (&q)[J], const RowView<T
     return count >= top;
 }
 
+// The largest key of the row below `below` (0: none), by one warp.
+template <typename T>
+__device__ __noinline__ uint64_t token_row_next(const RowView<T>& rv, uint64_t below) {
+    constexpr int n = RowView<T>::n;
+    uint64_t most = 0ull;
+    for (uint32_t v = threadIdx.x & 31u; v < rv.n_vec; v += 32u) {
+        const uint4 q = rv.load(v);
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const uint64_t x = order_key(elem<T>(q, i), rv.index(v, i));
+            if (x < below && rv.has(v, i)) most = max(most, x);
+        }
+    }
+    return warp_max_u64(most);
+}
+
 // Short rows: a warp per row, the row in registers (J vectors a lane).  The alternatives: the k-th largest of the 32
 // lanes' largest elements bounds the answer from below.  What reaches it -- on rows with many ties: what exceeds it,
 // and the first k that equal it -- is listed in shared memory and ranked by counting.  Rows that put too many elements
 // into the same lanes take k rounds of a maximum.
 template <typename T, int J>
-__global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const TokenArgs a) {
+__global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_kernel(const TokenArgs a) {
     constexpr int n = RowView<T>::n;
     __shared__ __align__(16) uint64_t s_key[TOK_ROW_WARPS][TOK_ROW_CAND];
+    __shared__ uint32_t s_where[TOK_ROW_WARPS][TOK_ROW_CAND];
     dep_wait();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint64_t r = (uint64_t)blockIdx.x * TOK_ROW_WARPS + warp;
@@ -306,32 +329,25 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const Tok
     const uint32_t all = __reduce_add_sync(0xFFFFFFFFu, mine);
     bool listed = all < TOK_ROW_CAND;
     if (listed) {
-        uint32_t* where = reinterpret_cast<uint32_t*>(key);
         uint32_t at = warp_sum_before(mine);
 #pragma unroll
         for (int i = 0; i < bits.words; ++i)
             for (uint32_t left = bits.w[i]; left; left &= left - 1u) {
                 const uint32_t p = bits.place(i, (uint32_t)__ffs((int)left) - 1u);
-                where[at++] = rv.index(lane + 32u * (p / n), (int)(p % n));
+                s_where[warp][at++] = rv.index(lane + 32u * (p / n), (int)(p % n));
             }
         __syncwarp();
-        uint64_t k[TOK_ROW_CAND / 32u];
-#pragma unroll
-        for (uint32_t i = 0; i < TOK_ROW_CAND / 32u; ++i) {
-            const uint32_t idx = i * 32u + lane < all ? where[i * 32u + lane] : a.V;
-            k[i] = idx < a.V ? order_key(to_f32(row[idx]), idx) : 0ull;      // a vector's foreign elements rank last
+        uint32_t real = 0;
+        for (uint32_t i = lane; i < ((all + 32u) & ~31u); i += 32u) {        // (and zeros behind the list)
+            const uint32_t idx = i < all ? s_where[warp][i] : a.V;
+            const bool is = idx < a.V;                                       // not a vector's foreign element
+            key[i] = is ? order_key(to_f32(row[idx]), idx) : 0ull;
+            real += __popc(__ballot_sync(0xFFFFFFFFu, is));
         }
         count = all;
-        __syncwarp();
-#pragma unroll
-        for (uint32_t i = 0; i < TOK_ROW_CAND / 32u; ++i)
-            if (i * 32u <= all) key[i * 32u + lane] = k[i];                  // (and zeros behind the list)
-        uint32_t real = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < TOK_ROW_CAND / 32u; ++i) real += k[i] != 0ull;
-        listed = __reduce_add_sync(0xFFFFFFFFu, real) >= top;                // NaN is not >= anything
+        listed = real >= top;                                                // NaN is not >= anything
     } else {
-        listed = token_row_ties<T, J>(q, rv, tau, top, key, count);
+        listed = token_row_ties<T>(rv, tau, top, key, count);
     }
     __syncwarp();
     if (listed) {
@@ -349,16 +365,7 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32) token_row_kernel(const Tok
     }
     uint64_t below = ~0ull;
     for (uint32_t k = 0; k < top; ++k) {
-        uint64_t most = 0ull;
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int i = 0; i < n; ++i)
-                if (rv.has(lane + 32u * j, i)) {
-                    const uint64_t x = order_key(elem<T>(q[j], i), rv.index(lane + 32u * j, i));
-                    if (x < below) most = max(most, x);
-                }
-        below = warp_max_u64(most);
+        below = token_row_next<T>(rv, below);
         if (lane == 0u) put_top(a, r, k, below, rs);
     }
 }
