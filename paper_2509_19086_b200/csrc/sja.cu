@@ -1604,6 +1604,9 @@ sja_status launch_token_stats(sja_ctx* c, const TokenArgs& a, uint32_t ctas) {
     return SJA_OK;
 }
 
+#ifndef TOK_MANY_ROWS
+#define TOK_MANY_ROWS 1000u
+#endif
 template <typename T>
 sja_status run_token_stats(sja_ctx* c, const TokenArgs& a) {
     constexpr uint32_t n = RowView<T>::n;
@@ -1616,7 +1619,7 @@ sja_status run_token_stats(sja_ctx* c, const TokenArgs& a) {
     // few rows: up to eight CTAs share one, as long as each thread has a vector
     uint32_t ctas = 1u;
     while (ctas < 8u && a.R * ctas * 2u <= (uint64_t)c->n_sm && vecs > ctas * 256u) ctas *= 2u;
-    if (vecs / ctas <= 1024u) return launch_token_stats<T, 128>(c, a, ctas);
+    if (vecs / ctas <= 1024u || a.R >= TOK_MANY_ROWS) return launch_token_stats<T, 128>(c, a, ctas);
     return launch_token_stats<T, 256>(c, a, ctas);
 }
 

@@ -1,8 +1,11 @@
 // Statistics of rows of logits: log probability of a given token, entropy, and the most likely alternatives.
 //
-// One pass keeps the largest logit m, the sum s = sum 2^d and the weighted sum w = sum 2^d d over d = (x - m) scale log2(e):
-// log p(v) = (x_v - m) scale - ln 2 log2 s, entropy = ln 2 (log2 s - w / s).  m is subtracted before anything is scaled,
-// so that a mask of the type's lowest value stays a (very small) number and a row of nothing else is uniform.
+// One pass keeps the largest logit m, the sum s = sum 2^d and the weighted sum w = sum 2^d d over d = x c - ref(m),
+// c = scale log2(e), ref(m) = m c rounded.  What ref rounds away is put back at the end:
+// log p(v) = (x_v - m) scale - ln 2 log2 s, entropy = ln 2 (log2 s - w / s), both with s relative to m c itself.
+// A logit whose product with c has no place in 32 bits (a mask of the type's lowest value) is -inf to the sums, as it
+// should be beside ordinary ones; where m itself is such a value, m is subtracted before anything is scaled, so that a
+// row of nothing else is uniform and not empty.
 #pragma once
 #include "sja_ssm.cuh"
 
@@ -35,29 +38,64 @@ __device__ __forceinline__ uint64_t order_key(float v, uint32_t idx) {
     return ((uint64_t)value_key(v) << 32) | (uint32_t)~idx;
 }
 
+// The same order for short rows: a 16-bit logit and a 16-bit index fit one 32-bit word.
+template <typename T> struct RowKey {
+    using K = uint64_t;
+    static __device__ __forceinline__ K make(T v, uint32_t idx) { return order_key(to_f32(v), idx); }
+    static __device__ __forceinline__ uint64_t wide(K k) { return k; }
+};
+template <typename T, uint32_t INF> struct RowKey16 {
+    using K = uint32_t;
+    static __device__ __forceinline__ K make(T v, uint32_t idx) {
+        uint32_t b = *reinterpret_cast<const uint16_t*>(&v);
+        if (b == 0x8000u) b = 0u;
+        const uint32_t code = (b & 0x7FFFu) > INF ? 0u : (b & 0x8000u) ? b ^ 0xFFFFu : b | 0x8000u;
+        return (code << 16) | (0xFFFFu - idx);
+    }
+    static __device__ __forceinline__ uint64_t wide(K k) {
+        if (!k) return 0ull;
+        const uint32_t code = k >> 16;
+        const uint16_t b = (uint16_t)((code & 0x8000u) ? code ^ 0x8000u : code ^ 0xFFFFu);
+        const float v = code ? to_f32(*reinterpret_cast<const T*>(&b)) : __uint_as_float(0x7FC00000u);
+        return order_key(v, 0xFFFFu - (k & 0xFFFFu));
+    }
+};
+template <> struct RowKey<__half> : RowKey16<__half, 0x7C00u> {};
+template <> struct RowKey<__nv_bfloat16> : RowKey16<__nv_bfloat16, 0x7F80u> {};
+
 // Sums of a part of a row relative to m (its largest logit; -inf where nothing was seen but -inf).
 struct Stat { float m, s, w; };
 
-__device__ __forceinline__ Stat stat_join(const Stat& a, const Stat& b, float c) {
-    Stat r;
-    r.m = fmaxf(a.m, b.m);
-    // an empty side has s = 0 (or NaN, which has to stay); inf - inf below is left to make NaN of a row with +inf
-    const float da = a.m == -INFINITY ? 0.0f : (a.m - r.m) * c, db = b.m == -INFINITY ? 0.0f : (b.m - r.m) * c;
-    const float fa = exp2_fast(da), fb = exp2_fast(db);
-    r.s = a.s * fa + b.s * fb;
-    r.w = fa * fmaf(a.s, fmaxf(da, -200.0f), a.w) + fb * fmaf(b.s, fmaxf(db, -200.0f), b.w);
-    return r;
+// (m c is far from the ends of the range; else differences are formed first)
+__device__ __forceinline__ bool scaled_fits(float m, float c) { return fabsf(m * c) < 1e37f; }
+// 2^(...) that takes sums relative to m into sums relative to a larger maximum
+__device__ __forceinline__ float stat_shift(float m, float larger, float c) {
+    if (m == -INFINITY) return 0.0f;                       // nothing was added up (or NaN was, which has to stay)
+    return scaled_fits(larger, c) ? m * c - larger * c : (m - larger) * c;
+}
+__device__ __forceinline__ void stat_move(Stat& a, float larger, float c) {
+    const float d = stat_shift(a.m, larger, c), f = exp2_fast(d);
+    a.w = f * fmaf(a.s, fmaxf(d, -200.0f), a.w);
+    a.s *= f;
+    a.m = larger;
+}
+__device__ __forceinline__ Stat stat_join(Stat a, Stat b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    stat_move(a, m, c);
+    stat_move(b, m, c);
+    return {m, a.s + b.s, a.w + b.w};
 }
 
 // Row log probabilities from the joined sums.
 struct RowStat {
     float m, log_s, entropy;
     __device__ __forceinline__ RowStat() {}
-    __device__ __forceinline__ explicit RowStat(const Stat& t) {
+    __device__ __forceinline__ RowStat(const Stat& t, float c) {
         const bool empty = t.m == -INFINITY && t.s == 0.0f;      // nothing but -inf
         m = empty ? 0.0f : t.m;
         log_s = empty ? 0.0f : __log2f(t.s);
         entropy = empty ? 0.0f : LN2 * (log_s - t.w / t.s);
+        if (scaled_fits(m, c)) log_s -= fmaf(m, c, -(m * c));
     }
     __device__ __forceinline__ float logp(float logit, float scale) const {
         if (logit == -INFINITY) return -INFINITY;
@@ -107,7 +145,8 @@ __device__ __forceinline__ float max_of(const uint4& q, __nv_bfloat16) {
     const __nv_bfloat162 m = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
     return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
 }
-template <typename T> __device__ __forceinline__ float elem(const uint4& q, int j) { return to_f32(reinterpret_cast<const T*>(&q)[j]); }
+template <typename T> __device__ __forceinline__ T raw(const uint4& q, int j) { return reinterpret_cast<const T*>(&q)[j]; }
+template <typename T> __device__ __forceinline__ float elem(const uint4& q, int j) { return to_f32(raw<T>(q, j)); }
 
 __device__ __forceinline__ Stat stat_shuffle(Stat st, uint32_t m) {
     Stat o;
@@ -117,22 +156,31 @@ __device__ __forceinline__ Stat stat_shuffle(Stat st, uint32_t m) {
     return o;
 }
 
-// Sums of vectors relative to m (a finite number, or +inf / NaN where the row has such), two elements at a time.
+// Adds a vector to sums relative to m (a finite number, or +inf / NaN where the row has such).
 template <typename T>
-__device__ __forceinline__ void add_vec(const uint4& q, F2 minus_m, F2 c, F2& s, F2& w) {
+__device__ __forceinline__ void add_vec(const uint4& q, float ref, float c, float (&s)[2], float (&w)[2]) {
 #pragma unroll
-    for (int j = 0; j < RowView<T>::n; j += 2) {
-        float d0, d1;
-        f2_split(f2_mul(f2_add(f2(elem<T>(q, j), elem<T>(q, j + 1)), minus_m), c), d0, d1);
-        const F2 e = f2(exp2_fast(d0), exp2_fast(d1));
-        s = f2_add(s, e);
-        w = f2_fma(e, f2(fmaxf(d0, -200.0f), fmaxf(d1, -200.0f)), w);    // 2^-200 is 0 here; -inf must not meet it
+    for (int j = 0; j < RowView<T>::n; ++j) {
+        const float d = fmaf(elem<T>(q, j), c, -ref), e = exp2_fast(d);
+        s[j & 1] += e;
+        w[j & 1] = fmaf(e, fmaxf(d, -200.0f), w[j & 1]);          // 2^-200 is 0 here; -inf must not meet it
     }
 }
-__device__ __forceinline__ float f2_sum(F2 v) {
-    float a, b;
-    f2_split(v, a, b);
-    return a + b;
+template <typename T, int J>
+__device__ __forceinline__ void add_vecs(const uint4 (&q)[J], float m, float c, float (&s)[2], float (&w)[2]) {
+    if (scaled_fits(m, c)) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) add_vec<T>(q[j], m * c, c, s, w);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < RowView<T>::n; ++i) {
+            const float d = (elem<T>(q[j], i) - m) * c, e = exp2_fast(d);
+            s[0] += e;
+            w[0] = fmaf(e, fmaxf(d, -200.0f), w[0]);
+        }
 }
 template <typename T> __device__ __forceinline__ uint4 empty_vec() {
     uint4 q;
@@ -179,15 +227,18 @@ template <typename T, int J> struct Bits {
     }
 };
 
-// Log probability of the row's token and entropy, by one thread.
-template <typename T>
-__device__ __forceinline__ void put_row(const TokenArgs& a, uint64_t r, const T* row, const RowStat& rs) {
-    if (a.entropy) a.entropy[r] = rs.entropy;
-    if (a.logp) {
-        const int64_t t = a.tokens[r];
-        a.logp[r] = t < 0 ? 0.0f : t >= (int64_t)a.V ? __uint_as_float(0x7FC00000u) : rs.logp(to_f32(row[t]), a.scale);
+// Log probability of the row's token and entropy, by one thread.  The token is looked up early: two loads that depend
+// on one another would otherwise end the row.
+template <typename T> struct RowToken {
+    int64_t t = -1;
+    float logit = 0.0f;
+    __device__ __forceinline__ RowToken(const TokenArgs& a, uint64_t r) { if (a.logp) t = __ldg(a.tokens + r); }
+    __device__ __forceinline__ void look(const TokenArgs& a, const T* row) { if (t >= 0 && t < (int64_t)a.V) logit = to_f32(row[t]); }
+    __device__ __forceinline__ void put(const TokenArgs& a, uint64_t r, const RowStat& rs) const {
+        if (a.entropy) a.entropy[r] = rs.entropy;
+        if (a.logp) a.logp[r] = t < 0 ? 0.0f : t >= (int64_t)a.V ? __uint_as_float(0x7FC00000u) : rs.logp(logit, a.scale);
     }
-}
+};
 // Alternative k of the row by its key; key 0: there is none.
 __device__ __forceinline__ void put_top(const TokenArgs& a, uint64_t r, uint32_t k, uint64_t key, const RowStat& rs) {
     if (a.top_ids) a.top_ids[r * a.top + k] = key ? (int32_t)~(uint32_t)key : -1;
@@ -224,7 +275,7 @@ __device__ __forceinline__ uint32_t warp_sum_before(uint32_t v) {
 // Rows in which too many elements reach the bound: those above it, and the first `top` that equal it in order of
 // index.  The row is read again (from the nearest cache).  False if even those above are too many, or NaN is needed.
 template <typename T>
-__device__ __noinline__ bool token_row_ties(const RowView<T>& rv, float tau, uint32_t top, uint64_t* key, uint32_t& count) {
+__device__ __noinline__ bool token_row_ties(const RowView<T>& rv, float tau, uint32_t top, typename RowKey<T>::K* key, uint32_t& count) {
     constexpr int n = RowView<T>::n;
     const uint32_t lane = threadIdx.x & 31u;
     uint32_t above = 0;
@@ -234,7 +285,7 @@ __device__ __noinline__ bool token_row_ties(const RowView<T>& rv, float tau, uin
         for (int i = 0; i < n; ++i) above += elem<T>(q, i) > tau;
     }
     const uint32_t above_all = __reduce_add_sync(0xFFFFFFFFu, above);
-    if (above_all > TOK_ROW_CAND - TOK_MAX_TOP) return false;
+    if (above_all > TOK_ROW_CAND - TOK_MAX_TOP - 4u) return false;
     uint32_t at = warp_sum_before(above), equal = 0;
     for (uint32_t v0 = 0; v0 < rv.n_vec; v0 += 32u) {
         const uint32_t v = v0 + lane;
@@ -243,20 +294,20 @@ __device__ __noinline__ bool token_row_ties(const RowView<T>& rv, float tau, uin
 #pragma unroll
         for (int i = 0; i < n; ++i) {
             const float x = elem<T>(q, i);
-            if (x > tau) key[at++] = order_key(x, rv.index(v, i));
+            if (x > tau) key[at++] = RowKey<T>::make(raw<T>(q, i), rv.index(v, i));
             mine += x == tau && rv.has(v, i);
         }
         uint32_t to = equal + warp_sum_before(mine);
 #pragma unroll
         for (int i = 0; i < n; ++i)
             if (elem<T>(q, i) == tau && rv.has(v, i)) {
-                if (to < top) key[above_all + to] = order_key(tau, rv.index(v, i));
+                if (to < top) key[above_all + to] = RowKey<T>::make(raw<T>(q, i), rv.index(v, i));
                 ++to;
             }
         equal += __reduce_add_sync(0xFFFFFFFFu, mine);
     }
     count = above_all + min(equal, top);
-    if ((count & 1u) && lane == 0u) key[count] = 0ull;       // the list is read in pairs
+    if (lane < 4u) key[count + lane] = 0;                    // the list is read in pieces of 16 bytes
     return count >= top;
 }
 
@@ -283,7 +334,9 @@ __device__ __noinline__ uint64_t token_row_next(const RowView<T>& rv, uint64_t b
 template <typename T, int J>
 __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_kernel(const TokenArgs a) {
     constexpr int n = RowView<T>::n;
-    __shared__ __align__(16) uint64_t s_key[TOK_ROW_WARPS][TOK_ROW_CAND];
+    using Key = RowKey<T>;
+    using K = typename Key::K;
+    __shared__ __align__(16) K s_key[TOK_ROW_WARPS][TOK_ROW_CAND];
     __shared__ uint32_t s_where[TOK_ROW_WARPS][TOK_ROW_CAND];
     dep_wait();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -291,9 +344,11 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_
     if (r >= a.R) return;
     const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
     const RowView<T> rv(row, a.V);
+    RowToken<T> token(a, r);
     uint4 q[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) q[j] = lane + 32u * j < rv.n_vec ? rv.load(lane + 32u * j) : empty_vec<T>();
+    token.look(a, row);
     float best = -INFINITY;
 #pragma unroll
     for (int j = 0; j < J; ++j) best = fmaxf(best, max_of(q[j], T()));
@@ -302,26 +357,24 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_
     for (uint32_t m = 16; m; m /= 2) st.m = fmaxf(st.m, __shfl_xor_sync(0xFFFFFFFFu, st.m, m));
     const float m0 = st.m == -INFINITY ? 0.0f : st.m;
     {
-        F2 ss = f2(0.0f, 0.0f), ww = ss;
-        const F2 nm = f2(-m0, -m0), cc = f2(a.c, a.c);
-#pragma unroll
-        for (int j = 0; j < J; ++j) add_vec<T>(q[j], nm, cc, ss, ww);
-        st.s = f2_sum(ss);
-        st.w = f2_sum(ww);
+        float ss[2] = {0.0f, 0.0f}, ww[2] = {0.0f, 0.0f};
+        add_vecs<T, J>(q, m0, a.c, ss, ww);
+        st.s = ss[0] + ss[1];
+        st.w = ww[0] + ww[1];
     }
 #pragma unroll
     for (uint32_t m = 16; m; m /= 2) {
         st.s += __shfl_xor_sync(0xFFFFFFFFu, st.s, m);
         st.w += __shfl_xor_sync(0xFFFFFFFFu, st.w, m);
     }
-    const RowStat rs(st);
-    if (lane == 0u) put_row(a, r, row, rs);
+    const RowStat rs(st, a.c);
+    if (lane == 0u) token.put(a, r, rs);
     if (!a.top) return;
     const uint32_t top = min(a.top, a.V);
     if (lane >= top && lane < a.top) put_top(a, r, lane, 0ull, rs);
     const float tau = __shfl_sync(0xFFFFFFFFu, warp_sort_desc(best), top - 1u);
 
-    uint64_t* key = s_key[warp];
+    K* key = s_key[warp];
     uint32_t count = 0;
     Bits<T, J> bits;
     bits.set(q, tau);
@@ -341,7 +394,7 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_
         for (uint32_t i = lane; i < ((all + 32u) & ~31u); i += 32u) {        // (and zeros behind the list)
             const uint32_t idx = i < all ? s_where[warp][i] : a.V;
             const bool is = idx < a.V;                                       // not a vector's foreign element
-            key[i] = is ? order_key(to_f32(row[idx]), idx) : 0ull;
+            key[i] = is ? Key::make(row[idx], idx) : 0;
             real += __popc(__ballot_sync(0xFFFFFFFFu, is));
         }
         count = all;
@@ -351,15 +404,18 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_
     }
     __syncwarp();
     if (listed) {
+        constexpr uint32_t piece = 16 / sizeof(K);
         for (uint32_t i = lane; i < count; i += 32u) {
-            const uint64_t k = key[i];
+            const K k = key[i];
             if (!k) continue;
             uint32_t rank = 0;
-            for (uint32_t o = 0; o < count; o += 2u) {
-                const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(key + o);
-                rank += (two.x > k) + (two.y > k);
+            for (uint32_t o = 0; o < count; o += piece) {
+                const uint4 w = *reinterpret_cast<const uint4*>(key + o);
+                const K* p = reinterpret_cast<const K*>(&w);
+#pragma unroll
+                for (uint32_t j = 0; j < piece; ++j) rank += p[j] > k;
             }
-            if (rank < top) put_top(a, r, rank, k, rs);
+            if (rank < top) put_top(a, r, rank, Key::wide(k), rs);
         }
         return;
     }
@@ -370,7 +426,7 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_
     }
 }
 
-constexpr uint32_t TOK_CAND = 1024, TOK_GROUPS = 16;
+constexpr uint32_t TOK_CAND = 1024, TOK_RANKED = 256, TOK_GROUPS = 16;
 
 // Long rows: a CTA per row, or a cluster of CTAs, each with a slice of the row, where there are few rows.  One sweep,
 // four vectors at a time, with a running maximum per thread.  The alternatives: every thread knows its largest
@@ -395,18 +451,25 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
     const RowView<T> rv(row, a.V);
     const uint32_t per = (rv.n_vec + n_rank - 1u) / n_rank, lo = min(rank * per, rv.n_vec), hi = min(lo + per, rv.n_vec);
     const uint32_t rounds = (per + THREADS * U - 1u) / (THREADS * U), stretch = (rounds + TOK_GROUPS - 1u) / TOK_GROUPS;
+    RowToken<T> token(a, r);
     if (tid == 0u) s_count = 0u;
 
     Stat st = {-INFINITY, 0.0f, 0.0f};
     uint32_t best_at = lo + tid;                                     // vector with the thread's first largest element
-    F2 ss = f2(0.0f, 0.0f), ww = ss;
-    const F2 cc = f2(a.c, a.c);
+    float ss[2] = {0.0f, 0.0f}, ww[2] = {0.0f, 0.0f};
     float group = -INFINITY;
-    for (uint32_t k = 0; k < rounds; ++k) {
+    for (uint32_t k = 0, in_group = 0, slot = 0; k < rounds; ++k) {
         const uint32_t v0 = lo + k * (THREADS * U) + tid;
         uint4 q[U];
+        const uint32_t first = lo + k * (THREADS * U);
+        if (first >= rv.whole_at && first + THREADS * U <= min(hi, rv.whole_at + rv.whole)) {
+            const uint4* p = reinterpret_cast<const uint4*>(rv.base) + v0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) q[u] = v0 + u * THREADS < hi ? rv.load(v0 + u * THREADS) : empty_vec<T>();
+            for (int u = 0; u < U; ++u) q[u] = __ldg(p + u * THREADS);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) q[u] = v0 + u * THREADS < hi ? rv.load(v0 + u * THREADS) : empty_vec<T>();
+        }
         float most = st.m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -416,20 +479,23 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
             group = fmaxf(group, vm);
         }
         // the sums so far move to the new maximum; without a branch, so that a warp stays together
-        const float m0 = most == -INFINITY ? 0.0f : most, d = st.m == -INFINITY ? 0.0f : (st.m - m0) * a.c, f = exp2_fast(d);
-        ww = f2_mul(f2(f, f), f2_fma(ss, f2(fmaxf(d, -200.0f), fmaxf(d, -200.0f)), ww));
-        ss = f2_mul(f2(f, f), ss);
-        st.m = most;
-        const F2 nm = f2(-m0, -m0);
+        const float m0 = most == -INFINITY ? 0.0f : most, d = stat_shift(st.m, m0, a.c), f = exp2_fast(d), dc = fmaxf(d, -200.0f);
 #pragma unroll
-        for (int u = 0; u < U; ++u) add_vec<T>(q[u], nm, cc, ss, ww);
-        if ((k + 1u) % stretch == 0u || k + 1u == rounds) {
-            s_group[k / stretch][tid] = group;
+        for (int i = 0; i < 2; ++i) {
+            ww[i] = f * fmaf(ss[i], dc, ww[i]);
+            ss[i] *= f;
+        }
+        st.m = most;
+        add_vecs<T, U>(q, m0, a.c, ss, ww);
+        if (++in_group == stretch || k + 1u == rounds) {
+            s_group[slot++][tid] = group;
             group = -INFINITY;
+            in_group = 0;
         }
     }
-    st.s = f2_sum(ss);
-    st.w = f2_sum(ww);
+    st.s = ss[0] + ss[1];
+    st.w = ww[0] + ww[1];
+    token.look(a, row);
     // the thread's largest key: the first element of that value in the vector where it first appeared
     uint64_t mine = 0ull;
     if (a.top && best_at < hi) {
@@ -457,8 +523,8 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
     for (int w = 1; w < WARPS; ++w) all = stat_join(all, s_stat[w], a.c);
     RowStat rs;
     if (n_rank == 1u) {
-        rs = RowStat(all);
-        if (tid == 0u) put_row(a, r, row, rs);
+        rs = RowStat(all, a.c);
+        if (tid == 0u) token.put(a, r, rs);
         if (!a.top) return;
         for (uint32_t k = top + tid; k < a.top; k += THREADS) put_top(a, r, k, 0ull, rs);
     }
@@ -471,13 +537,18 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
         for (int w = 1; w < WARPS; ++w) bound = min(bound, s_max[w]);
         uint32_t count;
         for (int attempt = 0;; ++attempt) {
-            const uint32_t bound_value = (uint32_t)(bound >> 32);
-            for (uint32_t k = 0; k < rounds; k += stretch) {
+            const uint32_t bound_value = (uint32_t)(bound >> 32), bound_index = ~(uint32_t)bound;
+            // whether a largest value found from vector v on can be part of the answer
+            auto reaches = [&](uint32_t value, uint32_t v) {
+                return value > bound_value || (value == bound_value && (v * n <= rv.skew || rv.index(v, 0) <= bound_index));
+            };
+            for (uint32_t k = 0, slot = 0; k < rounds; k += stretch, ++slot) {
                 // (a thread that met nothing but NaN has a maximum of -inf, above NaN's own place in the order)
-                if (value_key(s_group[k / stretch][tid]) < bound_value) continue;
-                for (uint32_t v = lo + k * (THREADS * U) + tid, i = 0; i < stretch * U && v < hi; ++i, v += THREADS) {
+                uint32_t v = lo + k * (THREADS * U) + tid;
+                if (!reaches(value_key(s_group[slot][tid]), v)) continue;
+                for (uint32_t i = 0; i < stretch * U && v < hi; ++i, v += THREADS) {
                     const uint4 q = rv.load(v);
-                    if (value_key(max_of(q, T())) < bound_value) continue;
+                    if (!reaches(value_key(max_of(q, T())), v)) continue;
 #pragma unroll
                     for (int j = 0; j < n; ++j) {
                         const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
@@ -490,7 +561,7 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
             }
             __syncthreads();
             count = s_count;
-            if (count <= TOK_CAND || attempt) break;
+            if (count <= TOK_RANKED || attempt) break;
             // many equal elements, or a warp with nothing large: the top-th largest of all threads' keys
             __syncthreads();
             s_cand[tid] = mine;
@@ -556,8 +627,8 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
     if (rank) return;
     all = s_part[0];
     for (uint32_t w = 1; w < n_rank; ++w) all = stat_join(all, s_part[w], a.c);
-    rs = RowStat(all);
-    if (tid == 0u) put_row(a, r, row, rs);
+    rs = RowStat(all, a.c);
+    if (tid == 0u) token.put(a, r, rs);
     const uint32_t want = min(a.top, a.V);
     for (uint32_t k = want + tid; k < a.top; k += THREADS) put_top(a, r, k, 0ull, rs);
     for (uint32_t i = tid; i < n_rank * a.top; i += THREADS) {
