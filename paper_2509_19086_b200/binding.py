@@ -151,12 +151,17 @@ def _ptr_space(a, space: Optional[int], np_dtype=None):
     return ptr, sp, keep
 
 
-_DTYPE_CODES = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+_torch_module = None
+_DTYPE_CODES: dict = {}          # torch dtype -> sja_dtype, filled when torch is first needed
 
 
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _DTYPE_CODES.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+        _torch_module = torch
+    return _torch_module
 
 
 class Sja:
@@ -169,7 +174,7 @@ class Sja:
         if st != SJA_OK:
             self._h = ctypes.c_void_p()
             raise SjaError(st, "sja_create failed (is a CUDA device present?)")
-        self.device, self.stream = int(device), int(stream or 0)
+        self.device, self.stream, self._torch_device = int(device), int(stream or 0), None
         self.n_jobs = 0
         self.n_gaps = 0
 
@@ -410,63 +415,70 @@ class Sja:
         ``entropy`` f32 (R,) in nats; with ``tokens`` (int64 (R,); negative = not scored, 0) their log
         probabilities ``logp`` f32 (R,); with ``top`` (up to 32) the most likely tokens ``top_ids`` i32 (R, top) in
         descending order, ties to the lowest, and their ``top_logp`` f32 (R, top)."""
+        torch = _torch()
         code = self._rows("logits", logits, None, None)
         R, V = logits.shape
         if tokens is not None:
-            self._flat("tokens", tokens, "int64", (R,))
-        a = SjaTokenRows(dtype=code, top=int(top), n_rows=R, vocab=V, scale=float(scale), logits=logits.data_ptr(),
-                         row_stride=max(logits.stride(0), V) if R < 2 else logits.stride(0))
-        torch, used = _torch(), (logits, tokens)
-        out = {"entropy": self._empty((R,), torch.float32, logits, used)}
-        a.entropy = out["entropy"].data_ptr()
+            self._flat("tokens", tokens, torch.int64, (R,))
+        top = int(top)
+        a = SjaTokenRows(code, top, R, V, scale, logits.data_ptr(), logits.stride(0) if R > 1 else V)
+        empty = self._allocator((logits, tokens))
+        entropy = empty((R,), torch.float32)
+        a.entropy = entropy.data_ptr()
+        out = {"entropy": entropy}
         if tokens is not None:
-            out["logp"] = self._empty((R,), torch.float32, logits, ())
-            a.tokens, a.logp = tokens.data_ptr(), out["logp"].data_ptr()
-        if 0 < top <= 32:
-            out["top_logp"] = self._empty((R, int(top)), torch.float32, logits, ())
-            out["top_ids"] = self._empty((R, int(top)), torch.int32, logits, ())
-            a.top_logp, a.top_ids = out["top_logp"].data_ptr(), out["top_ids"].data_ptr()
-        elif top == 0:
-            out["top_logp"] = self._empty((R, 0), torch.float32, logits, ())
-            out["top_ids"] = self._empty((R, 0), torch.int32, logits, ())
-        self._check(self._lib.sja_token_stats(self._h, ctypes.byref(a)))
+            out["logp"] = logp = empty((R,), torch.float32)
+            a.tokens, a.logp = tokens.data_ptr(), logp.data_ptr()
+        if 0 <= top <= 32:
+            out["top_logp"], out["top_ids"] = top_logp, top_ids = empty((R, top), torch.float32), empty((R, top), torch.int32)
+            a.top_logp, a.top_ids = top_logp.data_ptr(), top_ids.data_ptr()
+        st = self._lib.sja_token_stats(self._h, ctypes.byref(a))
+        if st:
+            self._check(st)
         return out
 
     def _rows(self, name, t, shape, dtype) -> int:
         """A CUDA tensor of rows (each contiguous) on this context's device; returns its sja_dtype."""
-        code = _DTYPE_CODES.get(str(getattr(t, "dtype", "")))
-        if code is None or not t.is_cuda or t.device.index != self.device:
+        if not _is_torch(t):
+            raise TypeError(f"{name}: a tensor on CUDA device {self.device} is needed")
+        _torch()
+        code = _DTYPE_CODES.get(t.dtype)
+        if code is None or not t.is_cuda or t.get_device() != self.device:
             raise TypeError(f"{name}: a float32, float16 or bfloat16 tensor on CUDA device {self.device} is needed")
         if dtype is not None and t.dtype != dtype:
             raise TypeError(f"{name}: {t.dtype}, where the rows are {dtype}")
-        if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        if t.dim() != 2 or (shape is not None and t.shape != shape):
             raise ValueError(f"{name}: shape {tuple(t.shape)}" + (f", not {shape}" if shape else " is not (rows, columns)"))
-        if t.shape[1] > 1 and t.stride(1) != 1:
+        if t.stride(1) != 1 and t.shape[1] > 1:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
         return code
 
     def _flat(self, name, t, dtype, shape) -> None:
         """A contiguous CUDA tensor of one type and shape (None in the shape: any length)."""
-        if not _is_torch(t) or str(t.dtype) != "torch." + dtype or not t.is_cuda or t.device.index != self.device:
+        if not _is_torch(t) or t.dtype != dtype or not t.is_cuda or t.get_device() != self.device:
             raise TypeError(f"{name}: a {dtype} tensor on CUDA device {self.device} is needed")
-        if t.dim() != len(shape) or any(w is not None and v != w for v, w in zip(t.shape, shape)):
+        if t.shape != shape and (t.dim() != len(shape) or any(w is not None and v != w for v, w in zip(t.shape, shape))):
             raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
         if not t.is_contiguous():
             raise ValueError(f"{name}: must be contiguous")
 
-    def _empty(self, shape, dtype, like, used):
-        """A new tensor for a result of this call.  Where torch works on another stream than the context, the memory
-        belongs to the context's stream, and the tensors the call uses are kept until that stream is through."""
+    def _allocator(self, used):
+        """What makes the tensors for a call's results.  Where torch works on another stream than the context, their
+        memory belongs to the context's stream, and the tensors the call uses are kept until that stream is through."""
         torch = _torch()
-        if torch.cuda.current_stream(self.device).cuda_stream == self.stream:
-            return torch.empty(shape, dtype=dtype, device=like.device)
+        if self._torch_device is None:
+            self._torch_device = torch.device("cuda", self.device)
+        if torch._C._cuda_getCurrentRawStream(self.device) == self.stream:
+            return lambda shape, dtype: torch.empty(shape, dtype=dtype, device=self._torch_device)
         mine = torch.cuda.ExternalStream(self.stream, device=self.device)
         for t in used:
             if t is not None:
                 t.record_stream(mine)
-        with torch.cuda.stream(mine):
-            out = torch.empty(shape, dtype=dtype, device=like.device)
-        return out
+
+        def empty(shape, dtype):
+            with torch.cuda.stream(mine):
+                return torch.empty(shape, dtype=dtype, device=self._torch_device)
+        return empty
 
     # -- sja_debug_fail_alloc
     def debug_fail_alloc(self, nth: int) -> None:
@@ -495,7 +507,8 @@ class SsmLayer:
     """
 
     def __init__(self, ctx: Sja, A, conv_w=None, conv_b=None, skip=None, dt_bias=None, n_groups: int = 1):
-        ctx._flat("A", A, "float32", (None, None))
+        torch = _torch()
+        ctx._flat("A", A, torch.float32, (None, None))
         D, N = A.shape
         G = int(n_groups)
         if G < 1 or D % G:
@@ -504,7 +517,7 @@ class SsmLayer:
         for name, t, shape in (("skip", skip, (D,)), ("dt_bias", dt_bias, (D,)), ("conv_w", conv_w, (rows, None)),
                                ("conv_b", conv_b, (rows,))):
             if t is not None:
-                ctx._flat(name, t, "float32", shape)
+                ctx._flat(name, t, torch.float32, shape)
         self.ctx, self.D, self.N, self.G, self.rows = ctx, D, N, G, rows
         self.W = 0 if conv_w is None else int(conv_w.shape[1])
         self._keep = (A, conv_w, conv_b, skip, dt_bias)
@@ -514,58 +527,64 @@ class SsmLayer:
 
     def _fill(self, xbc, dt, z, state, history, slots, n_jobs, out, more=()):
         """Check one call's tensors and write them into the call's arguments; returns (arguments, y)."""
-        ctx = self.ctx
-        code = ctx._rows("xbc", xbc, None, None)
-        T = xbc.shape[0]
+        ctx, torch = self.ctx, _torch()
+        a = SjaSsm.from_buffer_copy(self._args)
+        a.dtype = ctx._rows("xbc", xbc, None, None)
+        T, row_type = xbc.shape[0], xbc.dtype
         if xbc.shape[1] != self.rows:
             raise ValueError(f"xbc: rows of {xbc.shape[1]}, not D + 2GN = {self.rows}")
-        ctx._rows("dt", dt, (T, self.D), xbc.dtype)
+        shape = (T, self.D)
+        ctx._rows("dt", dt, shape, row_type)
+        a.xbc, a.dt = xbc.data_ptr(), dt.data_ptr()
         if z is not None:
-            ctx._rows("z", z, (T, self.D), xbc.dtype)
+            ctx._rows("z", z, shape, row_type)
+            a.z = z.data_ptr()
         n_slots = n_jobs
         if state is not None:
-            ctx._flat("state", state, "float32", (None, self.D, self.N))
+            ctx._flat("state", state, torch.float32, (None, self.D, self.N))
             n_slots = state.shape[0]
-        if history is not None:
-            ctx._flat("history", history, str(xbc.dtype)[6:], (None if state is None else n_slots, max(self.W - 1, 0), self.rows))
-            n_slots = history.shape[0]
-        if slots is not None:
-            ctx._flat("slots", slots, "int32", (n_jobs,))
-        if out is None:
-            out = ctx._empty((T, self.D), xbc.dtype, xbc, (xbc, dt, z, state, history, slots) + tuple(more))
-        else:
-            ctx._rows("out", out, (T, self.D), xbc.dtype)
-        a = SjaSsm.from_buffer_copy(self._args)
-        a.dtype, a.n_slots = code, n_slots
-        a.xbc, a.dt, a.y = xbc.data_ptr(), dt.data_ptr(), out.data_ptr()
-        a.xbc_stride, a.dt_stride, a.y_stride = xbc.stride(0), dt.stride(0), out.stride(0)
-        if z is not None:
-            a.z, a.z_stride = z.data_ptr(), z.stride(0)
-        if T < 2:                                       # the stride of a single row says nothing
-            a.xbc_stride, a.dt_stride, a.z_stride, a.y_stride = self.rows, self.D, self.D, self.D
-        if state is not None:
             a.state = state.data_ptr()
-        if history is not None and self.W > 1:
-            a.history = history.data_ptr()
+        if history is not None:
+            ctx._flat("history", history, row_type, (None if state is None else n_slots, max(self.W - 1, 0), self.rows))
+            n_slots = history.shape[0]
+            if self.W > 1:
+                a.history = history.data_ptr()
+        a.n_slots = n_slots
         if slots is not None:
+            ctx._flat("slots", slots, torch.int32, (n_jobs,))
             a.slots = slots.data_ptr()
+        if out is None:
+            out = ctx._allocator((xbc, dt, z, state, history, slots) + more)(shape, row_type)
+        else:
+            ctx._rows("out", out, shape, row_type)
+        a.y = out.data_ptr()
+        if T > 1:
+            a.xbc_stride, a.dt_stride, a.y_stride = xbc.stride(0), dt.stride(0), out.stride(0)
+            if z is not None:
+                a.z_stride = z.stride(0)
+        else:                                           # the stride of a single row says nothing
+            a.xbc_stride, a.dt_stride, a.z_stride, a.y_stride = self.rows, self.D, self.D, self.D
         return a, out
 
     def prompt(self, xbc, dt, off, state=None, history=None, z=None, slots=None, resume: bool = False, out=None):
         """sja_ssm_prompt: the packed tokens of S jobs, job s at rows ``off[s]`` .. ``off[s + 1] - 1`` (``off`` int64
         (S + 1,) on the device).  ``resume``: go on from the slots instead of from zero.  Returns y (T, D)."""
         ctx = self.ctx
-        ctx._flat("off", off, "int64", (None,))
+        ctx._flat("off", off, _torch().int64, (None,))
         S = off.shape[0] - 1
         if S < 0:
             raise ValueError("off: needs one entry per job and one more")
         a, y = self._fill(xbc, dt, z, state, history, slots, S, out, (off,))
-        ctx._check(ctx._lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), S, xbc.shape[0], off.data_ptr(), 1 if resume else 0))
+        st = ctx._lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), S, xbc.shape[0], off.data_ptr(), 1 if resume else 0)
+        if st:
+            ctx._check(st)
         return y
 
     def step(self, xbc, dt, state, history=None, z=None, slots=None, out=None):
         """sja_ssm_step: one token for each of S jobs, continued from and kept in their slots.  Returns y (S, D)."""
         ctx = self.ctx
         a, y = self._fill(xbc, dt, z, state, history, slots, xbc.shape[0], out)
-        ctx._check(ctx._lib.sja_ssm_step(ctx._h, ctypes.byref(a), xbc.shape[0]))
+        st = ctx._lib.sja_ssm_step(ctx._h, ctypes.byref(a), xbc.shape[0])
+        if st:
+            ctx._check(st)
         return y

@@ -1620,6 +1620,7 @@ sja_status run_token_stats(sja_ctx* c, const TokenArgs& a) {
     uint32_t ctas = 1u;
     while (ctas < 8u && a.R * ctas * 2u <= (uint64_t)c->n_sm && vecs > ctas * 256u) ctas *= 2u;
     if (vecs / ctas <= 1024u || a.R >= TOK_MANY_ROWS) return launch_token_stats<T, 128>(c, a, ctas);
+    if (ctas == 8u) return launch_token_stats<T, 512>(c, a, ctas);
     return launch_token_stats<T, 256>(c, a, ctas);
 }
 

@@ -254,7 +254,7 @@ __device__ __forceinline__ float warp_sort_desc(float v) {
         for (uint32_t j = k / 2; j > 0; j /= 2) {
             const float o = __shfl_xor_sync(0xFFFFFFFFu, v, j);
             const bool keep_max = ((lane & k) == 0u) == ((lane & j) == 0u);
-            v = keep_max ? fmaxf(v, o) : fminf(v, o);
+            v = (v > o) == keep_max ? v : o;                         // no NaN comes here
         }
     return v;
 }
@@ -426,21 +426,22 @@ __global__ void __launch_bounds__(TOK_ROW_WARPS * 32, J <= 4 ? 5 : 3) token_row_
     }
 }
 
-constexpr uint32_t TOK_CAND = 1024, TOK_RANKED = 256, TOK_GROUPS = 16;
+constexpr uint32_t TOK_CAND = 1024, TOK_RANKED = 256, TOK_GROUPS = 16, TOK_HITS = 512;
 
 // Long rows: a CTA per row, or a cluster of CTAs, each with a slice of the row, where there are few rows.  One sweep,
-// four vectors at a time, with a running maximum per thread.  The alternatives: every thread knows its largest
+// four vectors at a time (the next four on their way), with a running maximum per thread.  The alternatives: every thread knows its largest
 // element; the r-th largest of each warp's, r * warps >= top, bounds the slice's answer from below.  The sweep notes
-// the maximum of each stretch of a thread's vectors, so only stretches that reach the bound are read again.  The
-// candidates are ranked by counting, those of a cluster's slices once more in its first CTA.  Slices that keep too
-// many take `top` rounds of a maximum.
+// the maximum of each stretch of a thread's vectors; the stretches that reach the bound are listed and read again, a
+// vector per thread.  Their elements that reach it are ranked by counting, those of a cluster's slices once more in
+// its first CTA.  Where many do (equal elements, as in a row that a mask leaves empty), the top-th largest of all the
+// threads' elements is a second, exact bound; slices that still keep too many take `top` rounds of a maximum.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a) {
     constexpr int n = RowView<T>::n, WARPS = THREADS / 32, U = 4;
     __shared__ float s_group[TOK_GROUPS][THREADS];
     __shared__ uint64_t s_cand[TOK_CAND], s_top[8][TOK_MAX_TOP], s_max[WARPS];
     __shared__ Stat s_stat[WARPS], s_part[8];
-    __shared__ uint32_t s_count;
+    __shared__ uint32_t s_count, s_hits, s_hit[TOK_HITS];
     dep_wait();
     uint32_t rank, n_rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -452,24 +453,31 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
     const uint32_t per = (rv.n_vec + n_rank - 1u) / n_rank, lo = min(rank * per, rv.n_vec), hi = min(lo + per, rv.n_vec);
     const uint32_t rounds = (per + THREADS * U - 1u) / (THREADS * U), stretch = (rounds + TOK_GROUPS - 1u) / TOK_GROUPS;
     RowToken<T> token(a, r);
-    if (tid == 0u) s_count = 0u;
+    if (tid == 0u) s_count = s_hits = 0u;
 
     Stat st = {-INFINITY, 0.0f, 0.0f};
     uint32_t best_at = lo + tid;                                     // vector with the thread's first largest element
     float ss[2] = {0.0f, 0.0f}, ww[2] = {0.0f, 0.0f};
     float group = -INFINITY;
-    for (uint32_t k = 0, in_group = 0, slot = 0; k < rounds; ++k) {
-        const uint32_t v0 = lo + k * (THREADS * U) + tid;
-        uint4 q[U];
-        const uint32_t first = lo + k * (THREADS * U);
+    auto fetch = [&](uint4 (&to)[U], uint32_t k) {
+        const uint32_t first = lo + k * (THREADS * U), v0 = first + tid;
         if (first >= rv.whole_at && first + THREADS * U <= min(hi, rv.whole_at + rv.whole)) {
             const uint4* p = reinterpret_cast<const uint4*>(rv.base) + v0;
 #pragma unroll
-            for (int u = 0; u < U; ++u) q[u] = __ldg(p + u * THREADS);
+            for (int u = 0; u < U; ++u) to[u] = __ldg(p + u * THREADS);
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) q[u] = v0 + u * THREADS < hi ? rv.load(v0 + u * THREADS) : empty_vec<T>();
+            for (int u = 0; u < U; ++u) to[u] = v0 + u * THREADS < hi ? rv.load(v0 + u * THREADS) : empty_vec<T>();
         }
+    };
+    uint4 next[U];
+    fetch(next, 0);
+    for (uint32_t k = 0, in_group = 0, slot = 0; k < rounds; ++k) {
+        const uint32_t v0 = lo + k * (THREADS * U) + tid;
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u] = next[u];
+        if (k + 1u < rounds) fetch(next, k + 1u);
         float most = st.m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -544,28 +552,35 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
             };
             for (uint32_t k = 0, slot = 0; k < rounds; k += stretch, ++slot) {
                 // (a thread that met nothing but NaN has a maximum of -inf, above NaN's own place in the order)
-                uint32_t v = lo + k * (THREADS * U) + tid;
+                const uint32_t v = lo + k * (THREADS * U) + tid;
                 if (!reaches(value_key(s_group[slot][tid]), v)) continue;
-                for (uint32_t i = 0; i < stretch * U && v < hi; ++i, v += THREADS) {
-                    const uint4 q = rv.load(v);
-                    if (!reaches(value_key(max_of(q, T())), v)) continue;
+                const uint32_t at = atomicAdd(&s_hits, 1u);
+                if (at < TOK_HITS) s_hit[at] = v;
+            }
+            __syncthreads();
+            const uint32_t hits = s_hits;
+            for (uint32_t i = tid; hits <= TOK_HITS && i < hits * stretch * U; i += THREADS) {
+                const uint32_t v = s_hit[i / (stretch * U)] + i % (stretch * U) * THREADS;
+                if (v >= hi) continue;
+                const uint4 q = rv.load(v);
+                if (!reaches(value_key(max_of(q, T())), v)) continue;
 #pragma unroll
-                    for (int j = 0; j < n; ++j) {
-                        const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
-                        if (key >= bound && rv.has(v, j)) {
-                            const uint32_t at = atomicAdd(&s_count, 1u);
-                            if (at < TOK_CAND) s_cand[at] = key;
-                        }
+                for (int j = 0; j < n; ++j) {
+                    const uint64_t key = order_key(elem<T>(q, j), rv.index(v, j));
+                    if (key >= bound && rv.has(v, j)) {
+                        const uint32_t at = atomicAdd(&s_count, 1u);
+                        if (at < TOK_CAND) s_cand[at] = key;
                     }
                 }
             }
+            if (hits > TOK_HITS && tid == 0u) s_count = TOK_CAND + 1u;
             __syncthreads();
             count = s_count;
             if (count <= TOK_RANKED || attempt) break;
             // many equal elements, or a warp with nothing large: the top-th largest of all threads' keys
             __syncthreads();
             s_cand[tid] = mine;
-            if (tid == 0u) { s_count = 0u; s_max[0] = 0ull; }
+            if (tid == 0u) { s_count = 0u; s_hits = 0u; s_max[0] = 0ull; }
             __syncthreads();
             uint32_t place = 0;
             for (uint32_t j = 0; j < THREADS; ++j) place += s_cand[j] > mine;
