@@ -1459,7 +1459,8 @@ namespace {
 // Instance of the prompt kernel for N states: a lane holds up to 16 states of a channel, wider states are shared by 2,
 // 4 or 8 lanes.
 struct SsmShape { uint32_t K, lanes; uint32_t channels() const { return 32u / lanes; } };
-SsmShape ssm_shape(uint32_t N) {
+SsmShape ssm_shape(uint32_t N, bool few) {
+    if (few && N <= 16u) return {4u, 4u};
     if (N <= 8u) return {8u, 1u};
     if (N <= 16u) return {16u, 1u};
     if (N <= 32u) return {16u, 2u};
@@ -1469,7 +1470,8 @@ SsmShape ssm_shape(uint32_t N) {
 
 template <typename T, bool CARRY>
 void launch_ssm_prompt(const SsmShape& sh, dim3 grid, uint32_t threads, cudaStream_t stream, const SsmArgs& a) {
-    if (sh.K == 8u) launch_dep(ssm_prompt_kernel<T, 8, 1, CARRY>, grid, threads, 0, stream, a);
+    if (sh.K == 4u) launch_dep(ssm_prompt_kernel<T, 4, 4, CARRY>, grid, threads, 0, stream, a);
+    else if (sh.K == 8u) launch_dep(ssm_prompt_kernel<T, 8, 1, CARRY>, grid, threads, 0, stream, a);
     else if (sh.lanes == 1u) launch_dep(ssm_prompt_kernel<T, 16, 1, CARRY>, grid, threads, 0, stream, a);
     else if (sh.lanes == 2u) launch_dep(ssm_prompt_kernel<T, 16, 2, CARRY>, grid, threads, 0, stream, a);
     else if (sh.lanes == 4u) launch_dep(ssm_prompt_kernel<T, 16, 4, CARRY>, grid, threads, 0, stream, a);
@@ -1517,26 +1519,34 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
 #define SSM_WARPS_PER_SM 16u
 #endif
 #ifndef SSM_SNAP
-#define SSM_SNAP 2u
+#define SSM_SNAP 4u
+#endif
+#ifndef SSM_FEW
+#define SSM_FEW 65536u
+#endif
+#ifndef SSM_ONE_SEG
+#define SSM_ONE_SEG 128u
 #endif
 template <typename T>
 sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
     if (a.T > 0) {
-        const SsmShape sh = ssm_shape(a.N);
+        // A short prompt of few channels is bound by the time one warp takes for a token: four lanes share a channel.
+        const bool few = a.T * a.D <= SSM_FEW;
+        const SsmShape sh = ssm_shape(a.N, few);
         const uint32_t Dg = a.D / a.G, unit = sh.channels();
         const uint32_t need = (Dg + unit - 1u) / unit;                 // warps of one group's channels
         // the widest CTA that leaves the fewest warps without a channel (they share the tile of B and C)
-        uint32_t warps = SSM_THREADS / 32u;
+        uint32_t warps = few ? 1u : SSM_THREADS / 32u;
         while (warps > 1u && (need + warps - 1u) / warps * warps > (need + warps / 2u - 1u) / (warps / 2u) * (warps / 2u)) warps /= 2u;
         const uint32_t tiles = (need + warps - 1u) / warps * a.G;
         const uint64_t all = (uint64_t)need * a.G;
         uint64_t n_seg = std::max<uint64_t>(1, (uint64_t)c->n_sm * SSM_WARPS_PER_SM / all);
         n_seg = std::min<uint64_t>(n_seg, (a.T + 31u) / 32u);
-        if (n_seg < 3u && a.S == 1u) n_seg = 1u;                       // both passes over half the tokens gain nothing
+        if (a.T <= SSM_ONE_SEG || (n_seg < 3u && a.S == 1u)) n_seg = 1u;   // (two passes over half the tokens gain nothing)
         n_seg = std::min<uint64_t>(n_seg, 65535u);
         a.seg_len = (a.T + n_seg - 1u) / n_seg;
         a.n_seg = (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
-        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len / SSM_SNAP, 0x7FFFFFFFu);
+        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len * SSM_SNAP / 8u, 0x7FFFFFFFu);
         if (a.n_seg > 1u) {
             const size_t DN = (size_t)a.D * a.N, n = a.n_seg;
             const size_t h = n * DN * 4u, f = a.resume && a.state ? h : 0u, s = n * a.D * 4u;
@@ -1551,7 +1561,7 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         }
         launch_ssm_prompt<T, false>(sh, dim3(tiles, a.n_seg), warps * 32u, c->stream, a);
     }
-    if (a.state || (a.W > 1u && a.history))
+    if ((a.resume || a.T == 0) && (a.state || (a.W > 1u && a.history)))
         launch_dep(ssm_history_kernel<T>, dim3(a.S, (a.rows + 1023u) / 1024u), 256, 0, c->stream, a);
     CU(cudaGetLastError());
     return SJA_OK;

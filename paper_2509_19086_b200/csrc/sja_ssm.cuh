@@ -271,10 +271,40 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
         for (int i = 0; i < STRETCH; ++i) dst[i * (2 * NP)] = cv.next(a.W, v[i]);
     };
 
-    for (; t < b1 && s < a.S; ++s) {
+    // what a job leaves behind beside its state: its last W - 1 rows.  With `resume` other CTAs may still have to read
+    // the rows that these replace: then a kernel of its own stores them.
+    const bool keeps = !CARRY && !a.resume;
+    auto store_history = [&](uint64_t first, int64_t len, int64_t slot) {
+        if (a.W <= 1u || !a.history || slot < 0) return;
+        T* to = static_cast<T*>(a.history) + slot * (int64_t)(a.W - 1u) * a.rows;
+        for (uint32_t k = 0; k + 1u < a.W; ++k) {
+            const int64_t pos = len - (int64_t)(a.W - 1u) + k;
+            if (live && n0 == 0u) to[(uint64_t)k * a.rows + ch] = from_f32<T>(row_value<T>(a, first, pos, ch, slot));
+            if (blockIdx.x % tiles == 0u)
+                for (uint32_t i = tid; i < 2u * a.N; i += blockDim.x) {
+                    const uint32_t col = a.D + (i < a.N ? g * a.N + i : a.G * a.N + g * a.N + i - a.N);
+                    to[(uint64_t)k * a.rows + col] = from_f32<T>(row_value<T>(a, first, pos, col, slot));
+                }
+        }
+    };
+
+    // a segment has the jobs that end behind its first token and up to its end, empty ones among them
+    if (!CARRY && seg == 0u) s = 0u;
+    for (; s < a.S; ++s) {
         const uint64_t q = a.off[s];
         uint64_t e = a.off[s + 1u];
-        if (e <= t || q > t) continue;                 // an empty job (or offsets that are not ascending)
+        if (e == q && q <= b1) {
+            if (keeps) {
+                const int64_t slot = slot_of(a, s);
+#pragma unroll
+                for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
+                if (slot >= 0 && a.state) store_h(a.state + slot * (int64_t)DN);
+                store_history(q, 0, slot);
+            }
+            continue;
+        }
+        if (t >= b1 || q >= b1) break;
+        if (e <= t || q > t) continue;                 // offsets that are not ascending
         const bool ends = e <= b1;
         if (!ends) e = b1;
         const int64_t slot = slot_of(a, s);
@@ -322,16 +352,22 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
                     stage(w, q, slot, t + n_tok, (uint32_t)min((uint64_t)tile_tok, left - n_tok), s_bc[buf ^ 1u]);
             const float* bc = s_bc[buf] + n0;
             for (uint32_t i0 = 0; i0 < n_tok; i0 += U) {
-                float xv[U], dv[U], zv[U];
+                // convolution, time step and gate of the four tokens first: four independent chains (what follows a
+                // job's last token is worked out too, and not used)
+                float uv[U], dv[U], zv[U];
 #pragma unroll
-                for (int j = 0; j < U; ++j) { xv[j] = to_f32(xr[j]); dv[j] = to_f32(dr[j]); zv[j] = to_f32(zr[j]); }
+                for (int j = 0; j < U; ++j) {
+                    uv[j] = cx.next(a.W, to_f32(xr[j]));
+                    dv[j] = softplus(to_f32(dr[j]) + bias);
+                    zv[j] = CARRY || !a.z ? 1.0f : silu(to_f32(zr[j]));
+                }
                 px += U * a.xbc_stride; pd += U * a.dt_stride;
                 if (pz) pz += U * a.z_stride;
                 if (left > i0 + U) fetch(left - i0 - U);
 #pragma unroll
                 for (int j = 0; j < U; ++j) {
                     if (i0 + j >= n_tok) break;
-                    const float u = cx.next(a.W, xv[j]), d = softplus(dv[j] + bias);
+                    const float u = uv[j], d = dv[j];
                     if (CARRY) sdt += d;
                     const F2 d2 = f2(d, d), du2 = f2(d * u, d * u);
                     F2 acc = f2(0.0f, 0.0f);
@@ -359,7 +395,7 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
 #pragma unroll
                         for (int m = 1; m < LPC; m *= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
                         v = fmaf(skip, u, v);
-                        if (a.z) v *= silu(zv[j]);
+                        v *= zv[j];
                         if (live && n0 == 0u) py[j * a.y_stride] = from_f32<T>(v);
                     }
                 }
@@ -371,6 +407,7 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
             buf ^= 1u;
         }
         if (!CARRY && ends && slot >= 0 && a.state) store_h(a.state + slot * (int64_t)DN);
+        if (keeps && ends) store_history(q, (int64_t)(e - q), slot);
     }
     if (CARRY) {
         store_h(a.seg_h + (uint64_t)seg * DN);
@@ -396,8 +433,8 @@ __global__ void __launch_bounds__(256) ssm_carry_kernel(const SsmArgs a) {
     }
 }
 
-// What a prompt leaves behind beside the states: the last W - 1 rows of each job, and the zero state of a job without
-// tokens.  Behind the scan in the stream, because the scan of any CTA may read the rows kept before.
+// The last W - 1 rows of each job of a prompt that went on from its slots (or of one without any tokens, which also
+// leaves zero states).  Behind the scan in the stream, because the scan of any CTA may read the rows kept before.
 template <typename T>
 __global__ void __launch_bounds__(256) ssm_history_kernel(const SsmArgs a) {
     dep_wait();
