@@ -1456,29 +1456,35 @@ sja_status sja_get_scan(sja_ctx* c, uint64_t* boff, uint32_t* k, uint32_t* D, ui
 // Forecasting side: the recurrent scan of a sequence model, and the statistics of its answers.
 namespace {
 
-// Instance of the prompt kernel for N states: a lane holds up to 16 states of a channel, wider states are shared by 2,
-// 4 or 8 lanes.
-struct SsmShape { uint32_t K, lanes; uint32_t channels() const { return 32u / lanes; } };
+bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0; }
+
+#ifndef SSM_K32
+#define SSM_K32 16u
+#endif
+// Instance of the prompt kernel for N states: K of them in each of the lanes that share a channel.  One lane exchanges
+// nothing; four let a prompt of few tokens and channels through sooner, and hold wider states.
+struct SsmShape { uint32_t K, lanes; };
 SsmShape ssm_shape(uint32_t N, bool few) {
-    if (few && N <= 16u) return {4u, 4u};
-    if (N <= 8u) return {8u, 1u};
-    if (N <= 16u) return {16u, 1u};
-    if (N <= 32u) return {16u, 2u};
+    if (N <= 8u) return few ? SsmShape{2u, 4u} : SsmShape{8u, 1u};
+    if (N <= 16u) return few ? SsmShape{4u, 4u} : SsmShape{16u, 1u};
+    if (N <= 32u) return {8u, 4u};
     if (N <= 64u) return {16u, 4u};
-    return {16u, 8u};
+    return {32u, 4u};
 }
 
 template <typename T, bool CARRY>
 void launch_ssm_prompt(const SsmShape& sh, dim3 grid, uint32_t threads, cudaStream_t stream, const SsmArgs& a) {
-    if (sh.K == 4u) launch_dep(ssm_prompt_kernel<T, 4, 4, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.K == 8u) launch_dep(ssm_prompt_kernel<T, 8, 1, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.lanes == 1u) launch_dep(ssm_prompt_kernel<T, 16, 1, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.lanes == 2u) launch_dep(ssm_prompt_kernel<T, 16, 2, CARRY>, grid, threads, 0, stream, a);
-    else if (sh.lanes == 4u) launch_dep(ssm_prompt_kernel<T, 16, 4, CARRY>, grid, threads, 0, stream, a);
-    else launch_dep(ssm_prompt_kernel<T, 16, 8, CARRY>, grid, threads, 0, stream, a);
+    auto go = [&](auto kernel) { launch_dep(kernel, grid, threads, 0, stream, a); };
+    if (sh.lanes == 1u) {
+        if (sh.K == 8u) go(ssm_prompt_kernel<T, 8, 1, CARRY>);
+        else go(ssm_prompt_kernel<T, 16, 1, CARRY>);
+    } else if (sh.K == 2u) go(ssm_prompt_kernel<T, 2, 4, CARRY>);
+    else if (sh.K == 4u) go(ssm_prompt_kernel<T, 4, 4, CARRY>);
+    else if (sh.K == 8u) go(ssm_prompt_kernel<T, 8, 4, CARRY>);
+    else if (sh.K == 16u) go(ssm_prompt_kernel<T, 16, 4, CARRY>);
+    else go(ssm_prompt_kernel<T, 32, 4, CARRY>);
 }
 
-bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0; }
 size_t dtype_size(uint32_t dtype) { return dtype == SJA_F32 ? 4u : 2u; }
 
 // Argument checks shared by the two forms of the scan; fills the kernel arguments.
@@ -1497,6 +1503,8 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
     const int64_t rows = (int64_t)(D + 2 * G * N), d = (int64_t)D;
     if (m->xbc_stride < rows || m->dt_stride < d || m->y_stride < d || (m->z && m->z_stride < d))
         return fail(c, SJA_ERR_INVALID_ARG, "%s: a row stride is shorter than its row", who);
+    if (m->xbc_stride >= (1 << 28) || m->dt_stride >= (1 << 28) || m->y_stride >= (1 << 28) || (m->z && m->z_stride >= (1 << 28)))
+        return fail(c, SJA_ERR_INVALID_ARG, "%s: row strides reach 2^28 elements", who);
     const size_t e = dtype_size(m->dtype);
     if (!aligned_to(m->xbc, e) || !aligned_to(m->dt, e) || !aligned_to(m->z, e) || !aligned_to(m->y, e) || !aligned_to(m->history, e) ||
         !aligned_to(m->A, 4) || !aligned_to(m->skip, 4) || !aligned_to(m->dt_bias, 4) || !aligned_to(m->conv_w, 4) ||
@@ -1507,6 +1515,9 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
     a = SsmArgs();
     a.xbc = m->xbc; a.dt = m->dt; a.z = m->z; a.y = m->y;
     a.xbc_stride = m->xbc_stride; a.dt_stride = m->dt_stride; a.z_stride = m->z_stride; a.y_stride = m->y_stride;
+    const uint32_t el = (uint32_t)e;
+    a.xbc_bytes = (uint32_t)m->xbc_stride * el; a.dt_bytes = (uint32_t)m->dt_stride * el;
+    a.z_bytes = (uint32_t)m->z_stride * el; a.y_bytes = (uint32_t)m->y_stride * el;
     a.A = m->A; a.skip = m->skip; a.dt_bias = m->dt_bias; a.conv_w = m->conv_w; a.conv_b = m->conv_b;
     a.history = m->history; a.state = m->state; a.slots = m->slots;
     a.S = S; a.n_slots = m->n_slots; a.D = (uint32_t)D; a.N = (uint32_t)N; a.G = (uint32_t)G; a.W = m->conv_width;
@@ -1517,9 +1528,6 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
 // Warps an SM that a prompt aims at by splitting the token axis (16 of 128 registers fit).
 #ifndef SSM_WARPS_PER_SM
 #define SSM_WARPS_PER_SM 16u
-#endif
-#ifndef SSM_SNAP
-#define SSM_SNAP 4u
 #endif
 #ifndef SSM_FEW
 #define SSM_FEW 65536u
@@ -1533,7 +1541,7 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         // A short prompt of few channels is bound by the time one warp takes for a token: four lanes share a channel.
         const bool few = a.T * a.D <= SSM_FEW;
         const SsmShape sh = ssm_shape(a.N, few);
-        const uint32_t Dg = a.D / a.G, unit = sh.channels();
+        const uint32_t Dg = a.D / a.G, unit = 32u / sh.lanes;          // channels of a warp
         const uint32_t need = (Dg + unit - 1u) / unit;                 // warps of one group's channels
         // the widest CTA that leaves the fewest warps without a channel (they share the tile of B and C)
         uint32_t warps = few ? 1u : SSM_THREADS / 32u;
@@ -1543,10 +1551,11 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         uint64_t n_seg = std::max<uint64_t>(1, (uint64_t)c->n_sm * SSM_WARPS_PER_SM / all);
         n_seg = std::min<uint64_t>(n_seg, (a.T + 31u) / 32u);
         if (a.T <= SSM_ONE_SEG || (n_seg < 3u && a.S == 1u)) n_seg = 1u;   // (two passes over half the tokens gain nothing)
+        // about as many segments as jobs: then one each, which jobs of one length need not be cut for
+        if (a.S > 1u && 3ull * a.S >= 2u * n_seg && a.S <= 2u * n_seg) n_seg = a.S;
         n_seg = std::min<uint64_t>(n_seg, 65535u);
         a.seg_len = (a.T + n_seg - 1u) / n_seg;
         a.n_seg = (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
-        a.snap = (uint32_t)std::min<uint64_t>(a.seg_len * SSM_SNAP / 8u, 0x7FFFFFFFu);
         if (a.n_seg > 1u) {
             const size_t DN = (size_t)a.D * a.N, n = a.n_seg;
             const size_t h = n * DN * 4u, f = a.resume && a.state ? h : 0u, s = n * a.D * 4u;
@@ -1569,10 +1578,10 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
 
 template <typename T>
 sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
-    uint32_t lanes = 1u;
-    while (lanes * 4u < a.N) lanes *= 2u;
+    uint32_t log_lanes = 0u;
+    while ((4u << log_lanes) < a.N) ++log_lanes;
     const uint32_t vec = a.N % 4u == 0u && aligned16(a.A) && aligned16(a.state) ? 1u : 0u;
-    const size_t smem = (size_t)2u * a.G * lanes * 4u * sizeof(float);
+    const size_t smem = ((size_t)8u << log_lanes) * a.G * sizeof(float);
     // a job's channels are spread over up to eight CTAs (a portable cluster)
     const uint32_t ctas = std::min<uint32_t>(8u, (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS);
     cudaLaunchConfig_t cfg = {};
@@ -1581,13 +1590,13 @@ sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
     cfg.dynamicSmemBytes = smem;
     cfg.stream = c->stream;
     cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = ctas; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = ctas; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 2;
-    CU(cudaLaunchKernelEx(&cfg, ssm_step_kernel<T>, a, lanes, vec));
+    cfg.numAttrs = ctas > 1u ? 2u : 1u;
+    CU(vec ? cudaLaunchKernelEx(&cfg, ssm_step_kernel<T, true>, a, log_lanes) : cudaLaunchKernelEx(&cfg, ssm_step_kernel<T, false>, a, log_lanes));
     return SJA_OK;
 }
 

@@ -11,6 +11,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "sja_common.cuh"
 
 namespace sja {
@@ -22,6 +24,7 @@ struct SsmArgs {
     const void *xbc, *dt, *z;
     void* y;
     int64_t xbc_stride, dt_stride, z_stride, y_stride;   // elements between rows
+    uint32_t xbc_bytes, dt_bytes, z_bytes, y_bytes;      // the same in bytes (below 2^31)
     const float *A, *skip, *dt_bias, *conv_w, *conv_b;
     void* history;                // [n_slots, W - 1, rows] in the input type
     float* state;                 // [n_slots, D, N]
@@ -30,7 +33,7 @@ struct SsmArgs {
     uint64_t T;
     uint32_t S, n_slots, D, N, G, W, rows, resume;
     // split of the token axis (prompts)
-    uint32_t n_seg, snap;
+    uint32_t n_seg;
     uint64_t seg_len;
     uint32_t* seg_flag;           // [n_seg]
     float *seg_h, *seg_first, *seg_sdt;   // [n_seg, D, N], [n_seg, D, N], [n_seg, D]
@@ -116,29 +119,31 @@ __device__ __forceinline__ uint32_t warp_lower_bound(const uint64_t* __restrict_
     return lo;
 }
 
-// Boundary k of the token axis: k * seg_len, moved to the nearest start of a job when one is within `snap`
-// tokens.  A boundary between two jobs carries nothing over, so loads of jobs shorter than a segment never pay for
-// the split.
+// Boundary k of the token axis: k * seg_len, moved to the nearer end of the job it falls into when that job is not
+// longer than one and a half segments, or when that end is close.  A boundary between two jobs carries nothing over, so
+// loads of jobs of up to that length never pay for the split.
 __device__ __forceinline__ uint64_t segment_bound(const SsmArgs& a, uint32_t k) {
     if (k == 0u) return 0ull;
     if (k >= a.n_seg) return a.T;
     const uint64_t at = (uint64_t)k * a.seg_len;
     const uint32_t j = warp_lower_bound(a.off, a.S + 1u, at);
-    uint64_t best = at, dist = (uint64_t)a.snap + 1ull;
-    if (j <= a.S) {
-        const uint64_t v = a.off[j];
-        if (v - at < dist) { best = v; dist = v - at; }
-    }
-    if (j > 0u) {
-        const uint64_t v = a.off[j - 1u];
-        if (at - v < dist) best = v;
-    }
-    return best < a.T ? best : a.T;
+    if (j == 0u || j > a.S) return at < a.T ? at : a.T;
+    const uint64_t before = a.off[j - 1u], behind = a.off[j], down = at - before, up = behind - at;
+    const uint64_t near = down < up ? down : up;
+    if (near > (behind - before <= a.seg_len + a.seg_len / 2u ? a.seg_len : a.seg_len / 4u)) return at;
+    const uint64_t to = down < up ? before : behind;
+    return to < a.T ? to : a.T;
 }
 
 __device__ __forceinline__ int64_t slot_of(const SsmArgs& a, uint32_t s) {
     const int64_t v = a.slots ? (int64_t)a.slots[s] : (int64_t)s;
     return v >= 0 && v < (int64_t)a.n_slots ? v : -1;     // outside the pool: starts from zero, nothing is kept
+}
+
+// Row `rows` behind p, one multiply-add.
+template <typename P> __device__ __forceinline__ P* row_at(P* p, uint32_t rows, uint32_t bytes) {
+    using C = std::conditional_t<std::is_const_v<P>, const char, char>;
+    return reinterpret_cast<P*>(reinterpret_cast<C*>(p) + (uint64_t)rows * bytes);
 }
 
 // Raw row value of column `col` at position `pos` (counted from the job's first token of this call; negative
@@ -167,38 +172,62 @@ struct Conv {
         p2 = a.W > 2u ? row_value<T>(a, first, pos - 2, col, slot) : 0.0f;
         p3 = a.W > 3u ? row_value<T>(a, first, pos - 3, col, slot) : 0.0f;
     }
-    __device__ __forceinline__ float next(uint32_t W, float v) {
+    __device__ __forceinline__ float at(uint32_t W, float v, float v1, float v2, float v3) const {
         if (W == 0u) return v;
         float s = fmaf(w[3], v, b);
-        if (W > 1u) s = fmaf(w[2], p1, s);
-        if (W > 2u) s = fmaf(w[1], p2, s);
-        if (W > 3u) s = fmaf(w[0], p3, s);
-        p3 = p2; p2 = p1; p1 = v;
+        if (W > 1u) s = fmaf(w[2], v1, s);
+        if (W > 2u) s = fmaf(w[1], v2, s);
+        if (W > 3u) s = fmaf(w[0], v3, s);
         return silu(s);
+    }
+    __device__ __forceinline__ float next(uint32_t W, float v) {
+        const float u = at(W, v, p1, p2, p3);
+        p3 = p2; p2 = p1; p1 = v;
+        return u;
     }
 };
 
-constexpr uint32_t SSM_THREADS = 256;    // most threads of a prompt CTA
-// Tokens whose B and C one CTA keeps at a time: a thread convolves a stretch of 8 tokens of one column (2 NP of them).
-__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return 1024u / np; }
+// K consecutive values of shared memory as pairs.
+template <int K> __device__ __forceinline__ void load_pairs(F2 (&to)[K / 2], const float* from) {
+    if constexpr (K == 2) {
+        to[0].v = *reinterpret_cast<const unsigned long long*>(from);
+    } else {
+#pragma unroll
+        for (int k = 0; k < K / 4; ++k) {
+            const ulonglong2 q = reinterpret_cast<const ulonglong2*>(from)[k];
+            to[2 * k].v = q.x;
+            to[2 * k + 1].v = q.y;
+        }
+    }
+}
 
-// Prompts.  A thread owns one channel and K of its states (LPC lanes share a channel), walks its segment of the token
-// axis and keeps the states in registers.  B and C of a tile of tokens are convolved once per CTA into shared memory,
-// one tile ahead of the walk, and read by broadcast; x, dt and z of the next four tokens are on their way while four
-// are worked on.  CARRY = true is the first pass of a split: what the job that crosses the segment's end adds to its
-// state inside the segment, and its sum of time steps (exp(A sum dt) is the decay over the segment).
+#ifndef SSM_CTA
+#define SSM_CTA 256
+#endif
+constexpr uint32_t SSM_THREADS = SSM_CTA;    // most threads of a prompt CTA
+// Tokens whose B and C one CTA keeps at a time: a thread convolves a stretch of 8 tokens of one column (2 NP of them).
+__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np <= 64u ? 1024u / np : 16u; }
+
+// Prompts.  LPC lanes share a channel, K of its states each, and walk a segment of the token axis with the states in
+// registers, four tokens at a time: each lane works out convolution, time step and gate of its own share of the four
+// tokens (so that nothing is computed twice), all lanes advance their states through the four, and the partial sums
+// against C are exchanged so that a lane finishes and stores the tokens it began.  B and C of a tile of tokens are
+// convolved once per CTA into shared memory, one tile ahead of the walk; x, dt and z are P groups of four ahead.
+// CARRY = true is the first pass of a split: what the job that crosses the segment's end adds to its state inside the
+// segment, and its sum of time steps (exp(A sum dt) is the decay over the segment).
 template <typename T, int K, int LPC, bool CARRY>
-__global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArgs a) {
+__global__ void __launch_bounds__(SSM_THREADS, (LPC > 1 && K <= 8 ? 3 : 2) * 256 / SSM_THREADS) ssm_prompt_kernel(const SsmArgs a) {
     constexpr uint32_t NP = K * LPC, TT = ssm_tile_tokens(NP), CPW = 32 / LPC, COLS = CARRY ? NP : 2 * NP;
-    constexpr int U = 4, STRETCH = 8;
+    constexpr int U = 4, TPL = U / LPC, P = LPC, STRETCH = 8;
+    static_assert(LPC == 1 || LPC == 2 || LPC == 4, "four, two or one tokens a lane");
     __shared__ __align__(16) float s_bc[2][TT * 2 * NP];       // [buffer][token][B | C]
     dep_wait();
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, sub = lane % LPC;
     const uint32_t Dg = a.D / a.G, span = (blockDim.x >> 5) * CPW;
     const uint32_t tiles = (Dg + span - 1u) / span;
     const uint32_t g = blockIdx.x / tiles, seg = blockIdx.y;
     const uint32_t in_group = (blockIdx.x % tiles) * span + warp * CPW + lane / LPC;
-    const uint32_t n0 = (lane % LPC) * K;
+    const uint32_t n0 = sub * K;
     const bool live = in_group < Dg;
     const uint32_t ch = g * Dg + (live ? in_group : 0u);
     const uint64_t b0 = segment_bound(a, seg), b1 = segment_bound(a, seg + 1u);
@@ -241,14 +270,18 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
             if (live && n + 1u < a.N) r[n + 1u] = v1;
         }
     };
-    load_states(A2, a.A, LOG2E);
+    auto zero_h = [&]() {
 #pragma unroll
-    for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
+        for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
+    };
+    load_states(A2, a.A, LOG2E);
+    zero_h();
     const uint64_t DN = (uint64_t)a.D * a.N;
     const T* xp = static_cast<const T*>(a.xbc);
 
-    // this thread's part in convolving B and C: column bc_col, tokens bc_from .. bc_from + 7 of a tile
-    const uint32_t parts = max(blockDim.x / COLS, 1u), tile_tok = min(parts * (uint32_t)STRETCH, TT);
+    // this thread's part in convolving B and C: column w % COLS, tokens (w / COLS) * 8 .. + 7 of a tile
+    // (a tile is a whole number of prefetched groups: 16 tokens at least)
+    const uint32_t parts = max(blockDim.x / COLS, 2u), tile_tok = min(parts * (uint32_t)STRETCH, TT);
     auto stage = [&](uint32_t w, uint64_t q, int64_t slot, uint64_t at, uint32_t n_tok, float* to) {
         const uint32_t col = w % COLS, from = (w / COLS) * STRETCH, n = col % NP;
         if (from >= n_tok) return;
@@ -296,8 +329,7 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
         if (e == q && q <= b1) {
             if (keeps) {
                 const int64_t slot = slot_of(a, s);
-#pragma unroll
-                for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
+                zero_h();
                 if (slot >= 0 && a.state) store_h(a.state + slot * (int64_t)DN);
                 store_history(q, 0, slot);
             }
@@ -317,29 +349,38 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
             else load_states(h, a.seg_first + (uint64_t)seg * DN, 1.0f);
             if (CARRY) store_h(a.seg_first + (uint64_t)seg * DN);
         } else {
-#pragma unroll
-            for (int k = 0; k < K / 2; ++k) h[k] = f2(0.0f, 0.0f);
+            zero_h();
         }
-        cx.template seek<T>(a, q, (int64_t)(t - q), ch, slot);
-        const T* px = xp + (int64_t)t * a.xbc_stride + ch;
-        const T* pd = static_cast<const T*>(a.dt) + (int64_t)t * a.dt_stride + ch;
-        const T* pz = a.z && !CARRY ? static_cast<const T*>(a.z) + (int64_t)t * a.z_stride + ch : nullptr;
-        T* py = static_cast<T*>(a.y) + (int64_t)t * a.y_stride + ch;
-        uint64_t left = e - t;
-        T xr[U], dr[U], zr[U];
-        auto fetch = [&](uint64_t have) {              // rows behind the job's end are not touched
+        // this lane's tokens of each group of four are sub * TPL ..: pointers and prefetched values are theirs
+        float prev[TPL];
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                if ((uint64_t)j < have) {
-                    xr[j] = px[j * a.xbc_stride];
-                    dr[j] = pd[j * a.dt_stride];
-                    if (pz) zr[j] = pz[j * a.z_stride];
+        for (int i = 0; i < TPL; ++i) {
+            const int back = U - ((int)sub * TPL + i);             // tokens before t
+            prev[i] = back < (int)a.W ? row_value<T>(a, q, (int64_t)(t - q) - back, ch, slot) : 0.0f;
+        }
+        const uint64_t t_own = t + sub * TPL;
+        const T* px = xp + (int64_t)t_own * a.xbc_stride + ch;
+        const T* pd = static_cast<const T*>(a.dt) + (int64_t)t_own * a.dt_stride + ch;
+        const T* pz = a.z && !CARRY ? static_cast<const T*>(a.z) + (int64_t)t_own * a.z_stride + ch : nullptr;
+        T* py = static_cast<T*>(a.y) + (int64_t)t_own * a.y_stride + ch;
+        uint64_t left = e - t;
+        T xr[P][TPL], dr[P][TPL], zr[P][TPL];
+        // group `ahead` groups from the pointers, whose first token has `have` tokens of the job from it on
+        auto fetch = [&](int slot_p, int ahead, int32_t have) {
+#pragma unroll
+            for (int i = 0; i < TPL; ++i)
+                if ((int32_t)(sub * TPL + i) < have) {             // rows behind the job's end are not touched
+                    xr[slot_p][i] = *row_at(px, ahead * U + i, a.xbc_bytes);
+                    dr[slot_p][i] = *row_at(pd, ahead * U + i, a.dt_bytes);
+                    if (pz) zr[slot_p][i] = *row_at(pz, ahead * U + i, a.z_bytes);
                 }
-            }
         };
 #pragma unroll
-        for (int j = 0; j < U; ++j) xr[j] = dr[j] = zr[j] = from_f32<T>(0.0f);
-        fetch(left);
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+            for (int i = 0; i < TPL; ++i) xr[p][i] = dr[p][i] = zr[p][i] = from_f32<T>(0.0f);
+            fetch(p, p, (int32_t)min(left, (uint64_t)0x40000000u) - p * U);
+        }
         uint32_t buf = 0;
         __syncthreads();
         for (uint32_t w = tid; w < COLS * parts; w += blockDim.x)
@@ -351,55 +392,93 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
                 for (uint32_t w = tid; w < COLS * parts; w += blockDim.x)
                     stage(w, q, slot, t + n_tok, (uint32_t)min((uint64_t)tile_tok, left - n_tok), s_bc[buf ^ 1u]);
             const float* bc = s_bc[buf] + n0;
-            for (uint32_t i0 = 0; i0 < n_tok; i0 += U) {
-                // convolution, time step and gate of the four tokens first: four independent chains (what follows a
-                // job's last token is worked out too, and not used)
-                float uv[U], dv[U], zv[U];
+            const int32_t near = (int32_t)min(left, (uint64_t)0x40000000u);
+            auto group = [&](auto full, int p, uint32_t i0) {      // U tokens from i0 on, or fewer at the job's end
+                constexpr bool FULL = decltype(full)::value;
+                float cur[TPL], u[TPL], d[TPL], du[TPL], gate[TPL];
 #pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    uv[j] = cx.next(a.W, to_f32(xr[j]));
-                    dv[j] = softplus(to_f32(dr[j]) + bias);
-                    zv[j] = CARRY || !a.z ? 1.0f : silu(to_f32(zr[j]));
+                for (int i = 0; i < TPL; ++i) cur[i] = to_f32(xr[p][i]);
+                // the three values before this lane's first token
+                float b1v, b2v, b3v;
+                if constexpr (LPC == 4) {
+                    b1v = __shfl_sync(0xFFFFFFFFu, sub < 3u ? cur[0] : prev[0], (sub + 3u) % 4u, 4);
+                    b2v = __shfl_sync(0xFFFFFFFFu, sub < 2u ? cur[0] : prev[0], (sub + 2u) % 4u, 4);
+                    b3v = __shfl_sync(0xFFFFFFFFu, sub < 1u ? cur[0] : prev[0], (sub + 1u) % 4u, 4);
+                } else if constexpr (LPC == 1) {
+                    b1v = prev[TPL - 1]; b2v = prev[TPL - 2]; b3v = prev[TPL - 3];
+                } else {
+                    b1v = __shfl_xor_sync(0xFFFFFFFFu, sub == 0u ? cur[TPL - 1] : prev[TPL - 1], 1);
+                    b2v = __shfl_xor_sync(0xFFFFFFFFu, sub == 0u ? cur[0] : prev[0], 1);
+                    b3v = prev[TPL - 1];
                 }
-                px += U * a.xbc_stride; pd += U * a.dt_stride;
-                if (pz) pz += U * a.z_stride;
-                if (left > i0 + U) fetch(left - i0 - U);
+#pragma unroll
+                for (int i = 0; i < TPL; ++i) {
+                    u[i] = cx.at(a.W, cur[i], b1v, b2v, b3v);
+                    b3v = b2v; b2v = b1v; b1v = cur[i];
+                    d[i] = softplus(to_f32(dr[p][i]) + bias);
+                    du[i] = d[i] * u[i];
+                    gate[i] = CARRY || !a.z ? 1.0f : silu(to_f32(zr[p][i]));
+                    prev[i] = cur[i];
+                    if (CARRY && (FULL || i0 + sub * TPL + i < n_tok)) sdt += d[i];
+                }
+                fetch(p, P, near - (int32_t)i0 - P * U);
+                px = row_at(px, U, a.xbc_bytes);
+                pd = row_at(pd, U, a.dt_bytes);
+                if (pz) pz = row_at(pz, U, a.z_bytes);
+                float sum[U];
 #pragma unroll
                 for (int j = 0; j < U; ++j) {
-                    if (i0 + j >= n_tok) break;
-                    const float u = uv[j], d = dv[j];
-                    if (CARRY) sdt += d;
-                    const F2 d2 = f2(d, d), du2 = f2(d * u, d * u);
+                    sum[j] = 0.0f;
+                    const float dj = LPC == 1 ? d[j % TPL] : __shfl_sync(0xFFFFFFFFu, d[j % TPL], j / TPL, LPC);
+                    const float duj = LPC == 1 ? du[j % TPL] : __shfl_sync(0xFFFFFFFFu, du[j % TPL], j / TPL, LPC);
+                    if (!FULL && i0 + j >= n_tok) continue;
+                    const F2 d2 = f2(dj, dj), du2 = f2(duj, duj);
                     F2 acc = f2(0.0f, 0.0f);
-                    const ulonglong2* pB = reinterpret_cast<const ulonglong2*>(bc + (i0 + j) * (2 * NP));
+                    const float* row = bc + (i0 + j) * (2 * NP);
+                    F2 B2[K / 2], C2[K / 2];
+                    load_pairs<K>(B2, row);
+                    if (!CARRY) load_pairs<K>(C2, row + NP);
 #pragma unroll
-                    for (int k = 0; k < K / 4; ++k) {
-                        const ulonglong2 bq = pB[k];
-                        ulonglong2 cq = {0ull, 0ull};
-                        if (!CARRY) cq = pB[NP / 4 + k];
-                        const F2 b2[2] = {{bq.x}, {bq.y}}, c2[2] = {{cq.x}, {cq.y}};
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            float e0, e1;
-                            f2_split(f2_mul(d2, A2[2 * k + m]), e0, e1);
-                            const F2 decay = f2(exp2_fast(e0), exp2_fast(e1));
-                            F2& hh = h[2 * k + m];
-                            hh = f2_fma(decay, hh, f2_mul(du2, b2[m]));
-                            if (!CARRY) acc = f2_fma(hh, c2[m], acc);
-                        }
+                    for (int k = 0; k < K / 2; ++k) {
+                        float e0, e1;
+                        f2_split(f2_mul(d2, A2[k]), e0, e1);
+                        const F2 decay = f2(exp2_fast(e0), exp2_fast(e1));
+                        h[k] = f2_fma(decay, h[k], f2_mul(du2, B2[k]));
+                        if (!CARRY) acc = f2_fma(h[k], C2[k], acc);
                     }
-                    if (!CARRY) {
-                        float v0, v1;
-                        f2_split(acc, v0, v1);
-                        float v = v0 + v1;
-#pragma unroll
-                        for (int m = 1; m < LPC; m *= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
-                        v = fmaf(skip, u, v);
-                        v *= zv[j];
-                        if (live && n0 == 0u) py[j * a.y_stride] = from_f32<T>(v);
-                    }
+                    float v0, v1;
+                    f2_split(acc, v0, v1);
+                    sum[j] = v0 + v1;
                 }
-                py += U * a.y_stride;
+                if (!CARRY) {
+                    // each lane is left with the whole sums of its own tokens
+                    if constexpr (LPC == 4) {
+                        const bool high = sub & 2u;
+                        float k0 = high ? sum[2] : sum[0], k1 = high ? sum[3] : sum[1];
+                        k0 += __shfl_xor_sync(0xFFFFFFFFu, high ? sum[0] : sum[2], 2);
+                        k1 += __shfl_xor_sync(0xFFFFFFFFu, high ? sum[1] : sum[3], 2);
+                        const bool odd = sub & 1u;
+                        sum[0] = (odd ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, odd ? k0 : k1, 1);
+                    } else if constexpr (LPC == 2) {
+                        const bool odd = sub & 1u;
+                        const float k0 = (odd ? sum[2] : sum[0]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? sum[0] : sum[2], 1);
+                        const float k1 = (odd ? sum[3] : sum[1]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? sum[1] : sum[3], 1);
+                        sum[0] = k0; sum[1] = k1;
+                    }
+#pragma unroll
+                    for (int i = 0; i < TPL; ++i)
+                        if (live && (FULL || i0 + sub * TPL + i < n_tok))
+                            *row_at(py, i, a.y_bytes) = from_f32<T>(fmaf(skip, u[i], sum[i]) * gate[i]);
+                    py = row_at(py, U, a.y_bytes);
+                }
+            };
+            for (uint32_t i1 = 0; i1 < n_tok; i1 += U * P) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const uint32_t i0 = i1 + p * U;
+                    if (i0 + U <= n_tok) group(std::true_type{}, p, i0);
+                    else if (i0 < n_tok) group(std::false_type{}, p, i0);
+                }
             }
             // (a tile that is not a whole number of groups is the job's last one)
             t += n_tok;
@@ -411,6 +490,8 @@ __global__ void __launch_bounds__(SSM_THREADS, 2) ssm_prompt_kernel(const SsmArg
     }
     if (CARRY) {
         store_h(a.seg_h + (uint64_t)seg * DN);
+#pragma unroll
+        for (int m = 1; m < LPC; m *= 2) sdt += __shfl_xor_sync(0xFFFFFFFFu, sdt, m);
         if (live && n0 == 0u) a.seg_sdt[(uint64_t)seg * a.D + ch] = sdt;
     }
 }
@@ -465,56 +546,62 @@ constexpr uint32_t SSM_STEP_THREADS = 256;
 
 // Single tokens.  A CTA takes 256 channels of a job at a time: while their states are on the way (four 16-byte pieces
 // a thread), each thread works out convolution, time step and gate of one channel; then the states are advanced,
-// written back, and summed against C over the lanes of a channel.  The CTAs of a job form a cluster: each convolves
-// the job's B and C for itself, so the kept rows of B and C are replaced only when the whole cluster has read them.
-template <typename T>
-__global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const SsmArgs a, uint32_t lanes, uint32_t vec) {
+// written back, and summed against C over the 2^log_lanes lanes of a channel.  The CTAs of a job form a cluster: each
+// convolves the job's B and C for itself, so the kept rows of B and C are replaced only when the whole cluster has
+// read them.  VEC: N is a multiple of four and the states are aligned.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const SsmArgs a, uint32_t log_lanes) {
     extern __shared__ __align__(16) float s_bc[];           // B of all groups, then C, each padded to 4 * lanes
-    __shared__ float s_dt[SSM_STEP_THREADS], s_du[SSM_STEP_THREADS], s_y[SSM_STEP_THREADS];
-    constexpr int U = 4;
+    __shared__ float2 s_dd[SSM_STEP_THREADS];               // dt, dt u
+    __shared__ float s_y[SSM_STEP_THREADS];
+    constexpr uint32_t U = 4;
     dep_wait();
     uint32_t rank, n_rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_rank));
-    const uint32_t s = blockIdx.x / n_rank, tid = threadIdx.x, NP = 4u * lanes;
+    const uint32_t s = n_rank == 1u ? blockIdx.x : blockIdx.x / n_rank, tid = threadIdx.x;
     const int64_t slot = slot_of(a, s);
     const T* row = static_cast<const T*>(a.xbc) + (int64_t)s * a.xbc_stride;
-    const uint32_t H = a.W > 1u ? a.W - 1u : 0u;
+    const uint32_t H = a.W > 1u ? a.W - 1u : 0u, lanes = 1u << log_lanes;
     T* hist = H && a.history && slot >= 0 ? static_cast<T*>(a.history) + slot * (int64_t)H * a.rows : nullptr;
-    float* state = slot >= 0 && a.state ? a.state + slot * (int64_t)a.D * a.N : nullptr;
-    auto convolve = [&](uint32_t col, float v, float (&past)[3]) {
-#pragma unroll
-        for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H && hist ? to_f32(hist[(uint64_t)k * a.rows + col]) : 0.0f;
+    float* state = slot >= 0 ? a.state + slot * (int64_t)a.D * a.N : nullptr;
+    // the convolved value of a column, and the kept rows that it was made from
+    auto convolve = [&](uint32_t col, float v, T (&past)[3]) {
         if (a.W == 0u) return v;
+        const T* h = hist + col;
+#pragma unroll
+        for (uint32_t k = 0; k < 3u; ++k)
+            past[k] = k < H && hist ? *row_at(h, k, a.rows * (uint32_t)sizeof(T)) : from_f32<T>(0.0f);
         const float* w = a.conv_w + (uint64_t)col * a.W;
         float acc = fmaf(w[H], v, a.conv_b ? a.conv_b[col] : 0.0f);
 #pragma unroll
         for (uint32_t k = 0; k < 3u; ++k)
-            if (k < H) acc = fmaf(w[k], past[k], acc);
+            if (k < H) acc = fmaf(w[k], to_f32(past[k]), acc);
         return silu(acc);
     };
-    auto shift = [&](uint32_t col, float v, const float (&past)[3]) {
+    auto shift = [&](uint32_t col, T v, const T (&past)[3]) {
+        if (!hist) return;
+        T* h = hist + col;
 #pragma unroll
         for (uint32_t k = 0; k < 3u; ++k)
-            if (k < H && hist) hist[(uint64_t)k * a.rows + col] = from_f32<T>(k + 1u < H ? past[k < 2u ? k + 1u : 2u] : v);
+            if (k < H) *row_at(h, k, a.rows * (uint32_t)sizeof(T)) = k + 1u < H ? past[k < 2u ? k + 1u : 2u] : v;
     };
 
-    const uint32_t sub = tid % lanes, n = sub * 4u, per = SSM_STEP_THREADS / lanes, Dg = a.D / a.G;
+    const uint32_t sub = tid & (lanes - 1u), n = sub * 4u, mine = tid >> log_lanes, per = SSM_STEP_THREADS >> log_lanes;
     bool first = true;
     for (uint32_t base = rank * SSM_STEP_THREADS; base < a.D; base += n_rank * SSM_STEP_THREADS) {
+        const uint32_t here = min(a.D - base, SSM_STEP_THREADS);
         float4 hv[U], av[U];
         auto fetch = [&](uint32_t p0) {                     // passes p0 .. p0 + 3 over the 256 channels
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const uint32_t d = base + (p0 + j) * per + tid / lanes;
+            for (uint32_t j = 0; j < U; ++j) {
+                const uint32_t local = (p0 + j) * per + mine;
                 hv[j] = av[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (p0 + j >= lanes || d >= a.D) continue;
-                const uint64_t at = (uint64_t)d * a.N + n;
-                if (vec) {
-                    if (n < a.N) {
-                        if (state) hv[j] = *reinterpret_cast<const float4*>(state + at);
-                        av[j] = *reinterpret_cast<const float4*>(a.A + at);
-                    }
+                if (p0 + j >= lanes || local >= here || n >= a.N) continue;
+                const uint64_t at = (uint64_t)(base + local) * a.N + n;
+                if (VEC) {
+                    if (state) hv[j] = *reinterpret_cast<const float4*>(state + at);
+                    av[j] = __ldg(reinterpret_cast<const float4*>(a.A + at));
                 } else {
                     float* hq = &hv[j].x;
                     float* aq = &av[j].x;
@@ -530,21 +617,24 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const Ssm
         fetch(0);
         const uint32_t c = base + tid;
         float u = 0.0f, gate = 1.0f, skip = 0.0f;
-        if (c < a.D) {
-            const float xv = to_f32(row[c]);
-            float past[3];
-            u = convolve(c, xv, past);
-            shift(c, xv, past);
-            const float dt = softplus(to_f32(static_cast<const T*>(a.dt)[(int64_t)s * a.dt_stride + c]) + (a.dt_bias ? a.dt_bias[c] : 0.0f));
-            s_dt[tid] = dt;
-            s_du[tid] = dt * u;
-            if (a.z) gate = silu(to_f32(static_cast<const T*>(a.z)[(int64_t)s * a.z_stride + c]));
+        if (tid < here) {
+            const T xv = row[c];
+            const T dv = static_cast<const T*>(a.dt)[(int64_t)s * a.dt_stride + c];
+            T zv = from_f32<T>(0.0f), past[3];
+            if (a.z) zv = static_cast<const T*>(a.z)[(int64_t)s * a.z_stride + c];
             if (a.skip) skip = a.skip[c];
+            const float bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
+            u = convolve(c, to_f32(xv), past);
+            shift(c, xv, past);
+            const float dt = softplus(to_f32(dv) + bias);
+            s_dd[tid] = make_float2(dt, dt * u);
+            if (a.z) gate = silu(to_f32(zv));
         }
-        if (first)
-            for (uint32_t i = tid; i < 2u * a.G * NP; i += SSM_STEP_THREADS) {
-                const uint32_t m = i % NP, which = i / NP;  // which: B of group 0 .. G - 1, then C
-                float v = 0.0f, past[3];
+        if (first)                                          // B of group 0 .. G - 1, then C
+            for (uint32_t i = tid; i < 2u * a.G << (log_lanes + 2u); i += SSM_STEP_THREADS) {
+                const uint32_t m = i & (4u * lanes - 1u), which = i >> (log_lanes + 2u);
+                float v = 0.0f;
+                T past[3];
                 if (m < a.N) {
                     const uint32_t col = a.D + which * a.N + m;
                     v = convolve(col, to_f32(row[col]), past);
@@ -552,54 +642,59 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const Ssm
                 s_bc[i] = v;
             }
         __syncthreads();
-        if (first) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        if (first && n_rank > 1u) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
         first = false;
+        const uint32_t to_C = a.G << (log_lanes + 2u);
+        float4 B = *reinterpret_cast<const float4*>(s_bc + n), C = *reinterpret_cast<const float4*>(s_bc + n + to_C);
         for (uint32_t p0 = 0; p0 < lanes; p0 += U) {
             if (p0) fetch(p0);
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
+            for (uint32_t j = 0; j < U; ++j) {
                 if (p0 + j >= lanes) break;
-                const uint32_t local = (p0 + j) * per + tid / lanes, d = base + local;
-                const bool live = d < a.D;
-                const float dt = live ? s_dt[local] : 0.0f, du = live ? s_du[local] : 0.0f;
-                const float* bq = s_bc + (live ? d / Dg : 0u) * NP + n;
-                const float4 B = *reinterpret_cast<const float4*>(bq), C = *reinterpret_cast<const float4*>(bq + a.G * NP);
-                const float dl = dt * LOG2E;
-                hv[j].x = fmaf(exp2_fast(dl * av[j].x), hv[j].x, du * B.x);
-                hv[j].y = fmaf(exp2_fast(dl * av[j].y), hv[j].y, du * B.y);
-                hv[j].z = fmaf(exp2_fast(dl * av[j].z), hv[j].z, du * B.z);
-                hv[j].w = fmaf(exp2_fast(dl * av[j].w), hv[j].w, du * B.w);
+                const uint32_t local = (p0 + j) * per + mine;
+                const bool live = local < here;
+                const float2 dd = s_dd[live ? local : 0u];
+                if (a.G > 1u) {
+                    const float* bq = s_bc + n + (((live ? base + local : 0u) / (a.D / a.G)) << (log_lanes + 2u));
+                    B = *reinterpret_cast<const float4*>(bq);
+                    C = *reinterpret_cast<const float4*>(bq + to_C);
+                }
+                const float dl = dd.x * LOG2E;
+                hv[j].x = fmaf(exp2_fast(dl * av[j].x), hv[j].x, dd.y * B.x);
+                hv[j].y = fmaf(exp2_fast(dl * av[j].y), hv[j].y, dd.y * B.y);
+                hv[j].z = fmaf(exp2_fast(dl * av[j].z), hv[j].z, dd.y * B.z);
+                hv[j].w = fmaf(exp2_fast(dl * av[j].w), hv[j].w, dd.y * B.w);
                 float acc = fmaf(hv[j].x, C.x, hv[j].y * C.y) + fmaf(hv[j].z, C.z, hv[j].w * C.w);
                 for (uint32_t m = 1; m < lanes; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
-                if (live) {
-                    if (sub == 0u) s_y[local] = acc;
-                    const uint64_t at = (uint64_t)d * a.N + n;
-                    if (!state) continue;
-                    if (vec) {
-                        if (n < a.N) *reinterpret_cast<float4*>(state + at) = hv[j];
-                    } else {
-                        const float* hq = &hv[j].x;
+                if (!live) continue;
+                if (sub == 0u) s_y[local] = acc;
+                if (!state || n >= a.N) continue;
+                const uint64_t at = (uint64_t)(base + local) * a.N + n;
+                if (VEC) {
+                    *reinterpret_cast<float4*>(state + at) = hv[j];
+                } else {
+                    const float* hq = &hv[j].x;
 #pragma unroll
-                        for (uint32_t k = 0; k < 4u; ++k)
-                            if (n + k < a.N) state[at + k] = hq[k];
-                    }
+                    for (uint32_t k = 0; k < 4u; ++k)
+                        if (n + k < a.N) state[at + k] = hq[k];
                 }
             }
         }
         __syncthreads();
-        if (c < a.D)
-            static_cast<T*>(a.y)[(int64_t)s * a.y_stride + c] = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
-        // (s_y is next written behind the next round's barrier, s_dt and s_du are not read any more)
+        if (tid < here) static_cast<T*>(a.y)[(int64_t)s * a.y_stride + c] = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
+        // (s_y is next written behind the next round's barrier, s_dd is not read any more)
     }
-    if (first) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");   // a CTA without channels
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (n_rank > 1u) {
+        if (first) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");   // a CTA without channels
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
     if (rank == 0u && hist)
         for (uint32_t i = tid; i < 2u * a.G * a.N; i += SSM_STEP_THREADS) {
             const uint32_t col = a.D + i;
-            float past[3];
+            T past[3];
 #pragma unroll
-            for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H ? to_f32(hist[(uint64_t)k * a.rows + col]) : 0.0f;
-            shift(col, to_f32(row[col]), past);
+            for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H ? hist[(uint64_t)k * a.rows + col] : from_f32<T>(0.0f);
+            shift(col, row[col], past);
         }
 }
 
