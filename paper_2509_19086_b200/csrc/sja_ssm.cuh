@@ -642,7 +642,8 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const Ssm
                 s_bc[i] = v;
             }
         __syncthreads();
-        if (first && n_rank > 1u) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+        // (what was read is in shared memory: nothing has to be made visible to the others)
+        if (first && n_rank > 1u) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
         first = false;
         const uint32_t to_C = a.G << (log_lanes + 2u);
         float4 B = *reinterpret_cast<const float4*>(s_bc + n), C = *reinterpret_cast<const float4*>(s_bc + n + to_C);
@@ -685,7 +686,7 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const Ssm
         // (s_y is next written behind the next round's barrier, s_dd is not read any more)
     }
     if (n_rank > 1u) {
-        if (first) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");   // a CTA without channels
+        if (first) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // a CTA without channels
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
     if (rank == 0u && hist)
@@ -696,6 +697,147 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const Ssm
             for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H ? hist[(uint64_t)k * a.rows + col] : from_f32<T>(0.0f);
             shift(col, row[col], past);
         }
+}
+
+// Single tokens of many jobs.  B and C first, once per job: convolved into the workspace, their kept rows replaced.
+template <typename T>
+__global__ void __launch_bounds__(256) ssm_step_bc_kernel(const SsmArgs a, uint32_t np, float* __restrict__ bc) {
+    dep_wait();
+    const uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const uint32_t width = 2u * a.G * np, s = (uint32_t)(i / width), k = (uint32_t)(i % width);
+    if (s >= a.S) return;
+    const uint32_t m = k % np;
+    float v = 0.0f;
+    if (m < a.N) {
+        const uint32_t col = a.D + k / np * a.N + m, H = a.W > 1u ? a.W - 1u : 0u;
+        const int64_t slot = slot_of(a, s);
+        const T x = static_cast<const T*>(a.xbc)[(int64_t)s * a.xbc_stride + col];
+        T* h = H && a.history && slot >= 0 ? static_cast<T*>(a.history) + slot * (int64_t)H * a.rows + col : nullptr;
+        T past[3];
+#pragma unroll
+        for (uint32_t j = 0; j < 3u; ++j) past[j] = j < H && h ? h[(uint64_t)j * a.rows] : from_f32<T>(0.0f);
+        Conv cv;
+        cv.load(a, col);
+        const float f0 = to_f32(past[0]), f1 = to_f32(past[1]), f2v = to_f32(past[2]);
+        v = cv.at(a.W, to_f32(x), H == 1u ? f0 : H == 2u ? f1 : f2v, H == 2u ? f0 : f1, f0);
+        if (h) {
+#pragma unroll
+            for (uint32_t j = 0; j < 3u; ++j)
+                if (j < H) h[(uint64_t)j * a.rows] = j + 1u < H ? past[j < 2u ? j + 1u : 2u] : x;
+        }
+    }
+    bc[i] = v;
+}
+
+__device__ __forceinline__ void copy_async16(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+
+// Then the states: a CTA keeps to 256 channels and goes from job to job, with the states of the next STAGES - 1 jobs on
+// their way into shared memory and the rows of the next one in registers, so that the memory never waits for a job's
+// arithmetic.
+template <typename T, int STAGES>
+__global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(const SsmArgs a, uint32_t log_lanes, const float* __restrict__ bc) {
+    extern __shared__ __align__(16) float s_state[];        // [STAGES][256 channels][N]
+    __shared__ __align__(16) float s_bc[SSM_STEP_THREADS];  // B of group 0 .. G - 1, then C, each padded to 4 * lanes
+    __shared__ float2 s_dd[SSM_STEP_THREADS];               // dt, dt u
+    __shared__ float s_y[SSM_STEP_THREADS];
+    dep_wait();
+    const uint32_t tid = threadIdx.x, lanes = 1u << log_lanes, base = blockIdx.x * SSM_STEP_THREADS, step = gridDim.y;
+    const uint32_t here = min(a.D - base, SSM_STEP_THREADS), H = a.W > 1u ? a.W - 1u : 0u;
+    const uint32_t sub = tid & (lanes - 1u), n = sub * 4u, mine = tid >> log_lanes, per = SSM_STEP_THREADS >> log_lanes;
+    const uint32_t width = 2u * a.G << (log_lanes + 2u), to_C = width / 2u, stage = SSM_STEP_THREADS * a.N, hist_row = a.rows * (uint32_t)sizeof(T);
+    const uint32_t c = base + min(tid, here - 1u);
+    Conv cv;
+    cv.load(a, c);
+    const float skip = a.skip ? a.skip[c] : 0.0f, bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
+    const uint64_t DN = (uint64_t)a.D * a.N;
+    auto slot_at = [&](uint32_t s) { return s < a.S ? slot_of(a, s) : (int64_t)-1; };
+    // this thread's 16-byte pieces of the tile are the ones it works on later, so that it waits for its own only
+    auto start = [&](uint32_t to, int64_t slot) {
+        if (slot >= 0 && n < a.N)
+            for (uint32_t p = 0; p < lanes; ++p) {
+                const uint32_t local = p * per + mine;
+                if (local < here) copy_async16(s_state + to * stage + local * a.N + n, a.state + (uint64_t)slot * DN + (uint64_t)(base + local) * a.N + n);
+            }
+        copy_commit();
+    };
+    T xv, dv, zv, past[3];
+    float bcv = 0.0f;
+    T* hist = nullptr;
+    auto fetch = [&](uint32_t s, int64_t slot) {
+        hist = H && a.history && slot >= 0 ? static_cast<T*>(a.history) + slot * (int64_t)H * a.rows + c : nullptr;
+        if (s >= a.S) return;
+        xv = static_cast<const T*>(a.xbc)[(int64_t)s * a.xbc_stride + c];
+        dv = static_cast<const T*>(a.dt)[(int64_t)s * a.dt_stride + c];
+        if (a.z) zv = static_cast<const T*>(a.z)[(int64_t)s * a.z_stride + c];
+#pragma unroll
+        for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H && hist ? *row_at(hist, k, hist_row) : from_f32<T>(0.0f);
+        if (tid < width) bcv = bc[(uint64_t)s * width + tid];
+    };
+    uint32_t s = blockIdx.y;
+    int64_t slots[STAGES];                                  // of this job and the next ones
+#pragma unroll
+    for (uint32_t i = 0; i < (uint32_t)STAGES; ++i) slots[i] = slot_at(s + i * step);
+#pragma unroll
+    for (uint32_t i = 0; i + 1u < (uint32_t)STAGES; ++i) start(i, slots[i]);
+    fetch(s, slots[0]);
+    uint32_t at = 0;
+    for (; s < a.S; s += step) {
+        start(at == 0u ? STAGES - 1u : at - 1u, slots[STAGES - 1]);     // its stage was emptied by the job before
+        // convolution, time step and gate of one channel
+        float gate = 1.0f;
+        const float f0 = to_f32(past[0]), f1 = to_f32(past[1]), f2v = to_f32(past[2]);
+        const float u = cv.at(a.W, to_f32(xv), H == 1u ? f0 : H == 2u ? f1 : f2v, H == 2u ? f0 : f1, f0);
+        if (hist && tid < here) {
+#pragma unroll
+            for (uint32_t k = 0; k < 3u; ++k)
+                if (k < H) *row_at(hist, k, hist_row) = k + 1u < H ? past[k < 2u ? k + 1u : 2u] : xv;
+        }
+        const float dt = softplus(to_f32(dv) + bias);
+        s_dd[tid] = make_float2(dt, dt * u);
+        if (a.z) gate = silu(to_f32(zv));
+        if (tid < width) s_bc[tid] = bcv;
+        fetch(s + step, slots[1]);
+        copy_wait<STAGES - 1>();
+        __syncthreads();
+        const float* tile = s_state + at * stage;
+        float* state = slots[0] >= 0 ? a.state + (uint64_t)slots[0] * DN : nullptr;
+        float4 B = *reinterpret_cast<const float4*>(s_bc + n), C = *reinterpret_cast<const float4*>(s_bc + n + to_C);
+#pragma unroll 4
+        for (uint32_t p = 0; p < lanes; ++p) {
+            const uint32_t local = p * per + mine;
+            const bool live = local < here && n < a.N;
+            const uint32_t el = live ? local * a.N + n : 0u;
+            const float2 dd = s_dd[local];
+            if (a.G > 1u) {
+                const float* bq = s_bc + n + (((live ? base + local : 0u) / (a.D / a.G)) << (log_lanes + 2u));
+                B = *reinterpret_cast<const float4*>(bq);
+                C = *reinterpret_cast<const float4*>(bq + to_C);
+            }
+            float4 h = state && live ? *reinterpret_cast<const float4*>(tile + el) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            const float4 A = __ldg(reinterpret_cast<const float4*>(a.A + (uint64_t)base * a.N + el));
+            const float dl = dd.x * LOG2E;
+            h.x = fmaf(exp2_fast(dl * A.x), h.x, dd.y * B.x);
+            h.y = fmaf(exp2_fast(dl * A.y), h.y, dd.y * B.y);
+            h.z = fmaf(exp2_fast(dl * A.z), h.z, dd.y * B.z);
+            h.w = fmaf(exp2_fast(dl * A.w), h.w, dd.y * B.w);
+            float acc = fmaf(h.x, C.x, h.y * C.y) + fmaf(h.z, C.z, h.w * C.w);
+            if (n >= a.N) acc = 0.0f;
+            for (uint32_t m = 1; m < lanes; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
+            if (sub == 0u) s_y[local] = acc;
+            if (state && live) *reinterpret_cast<float4*>(state + (uint64_t)base * a.N + el) = h;
+        }
+        __syncthreads();
+        if (tid < here) static_cast<T*>(a.y)[(int64_t)s * a.y_stride + c] = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
+#pragma unroll
+        for (int i = 0; i + 1 < STAGES; ++i) slots[i] = slots[i + 1];
+        slots[STAGES - 1] = slot_at(s + STAGES * step);
+        at = at + 1u == (uint32_t)STAGES ? 0u : at + 1u;
+    }
+    copy_wait<0>();
 }
 
 }  // namespace sja

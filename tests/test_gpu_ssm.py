@@ -141,7 +141,9 @@ def test_prompt_in_pieces_and_by_single_tokens(ctx):
 
 @pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
 @pytest.mark.parametrize("shape", [(1, 1, 1, 1, 1), (1, 300, 16, 1, 4), (3, 70, 16, 2, 4), (5, 33, 7, 3, 2), (2, 20, 128, 1, 3),
-                                   (400, 40, 32, 1, 4), (7, 500, 64, 4, 0), (2, 9, 3, 1, 4)], ids=str)
+                                   (400, 40, 32, 1, 4), (7, 500, 64, 4, 0), (2, 9, 3, 1, 4),
+                                   (700, 260, 16, 1, 4), (900, 30, 12, 2, 3), (601, 64, 64, 2, 4), (1300, 5, 4, 5, 1),
+                                   (650, 300, 8, 3, 2), (620, 17, 32, 1, 0)], ids=str)
 def test_step(ctx, shape, dtype):
     S, D, N, G, W = shape
     c = Case([1] * S, D, N, G, W, dtype, gate=D % 2 == 0, seed=S + D, n_slots=S + 2)
