@@ -356,14 +356,13 @@ cudaError_t sorted_smem_attr() {
                                 TILE_SMEM_BYTES);
 }
 
-// sja_ssm_step: the stages of a persistent CTA (up to 32 states a channel: three; up to 64: two).
-template <typename T>
+// sja_ssm_step: the stages of a persistent CTA, for the most states of an instance.
+template <typename T, int LOG>
 cudaError_t ssm_smem_attr() {
-    const cudaError_t e = cudaFuncSetAttribute(ssm_step_many_kernel<T, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               3 * SSM_STEP_THREADS * 32 * (int)sizeof(float));
-    if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(ssm_step_many_kernel<T, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                2 * SSM_STEP_THREADS * 64 * (int)sizeof(float));
+    const cudaError_t e = cudaFuncSetAttribute(ssm_step_many_kernel<T, LOG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               ssm_step_stages<LOG>() * (int)SSM_STEP_THREADS * (4 << LOG) * (int)sizeof(float));
+    if constexpr (LOG > 0) return e == cudaSuccess ? ssm_smem_attr<T, LOG - 1>() : e;
+    return e;
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -614,8 +613,8 @@ sja_status sja_create(sja_ctx** out, int device, void* cuda_stream) {
             st = SJA_ERR_CUDA;
             break;
         }
-        if (ssm_smem_attr<float>() != cudaSuccess || ssm_smem_attr<__half>() != cudaSuccess ||
-            ssm_smem_attr<__nv_bfloat16>() != cudaSuccess) { st = SJA_ERR_CUDA; break; }
+        if (ssm_smem_attr<float, 4>() != cudaSuccess || ssm_smem_attr<__half, 4>() != cudaSuccess ||
+            ssm_smem_attr<__nv_bfloat16, 4>() != cudaSuccess) { st = SJA_ERR_CUDA; break; }
         if ((st = reserve(c, c->gap_info, sizeof(GapInfo))) != SJA_OK) break;
     } while (0);
     if (st != SJA_OK) {
@@ -1591,17 +1590,16 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
 #ifndef SSM_STEP_MANY
 #define SSM_STEP_MANY 4u
 #endif
-template <typename T, int STAGES>
-sja_status launch_ssm_step_many(sja_ctx* c, const SsmArgs& a, uint32_t log_lanes) {
-    const uint32_t np = 4u << log_lanes, tiles = (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS;
+template <typename T, int LOG>
+sja_status launch_ssm_step_many(sja_ctx* c, const SsmArgs& a) {
+    const uint32_t np = 4u << LOG, tiles = (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS;
     const uint64_t values = (uint64_t)a.S * 2u * a.G * np;
     TRY(reserve(c, c->ssm_ws, values * sizeof(float)));
     launch_dep(ssm_step_bc_kernel<T>, dim3((uint32_t)((values + 255u) / 256u)), 256, 0, c->stream, a, np, c->ssm_ws.as<float>());
-    const uint32_t smem = STAGES * SSM_STEP_THREADS * a.N * sizeof(float);
-    auto kernel = ssm_step_many_kernel<T, STAGES>;
-    const uint32_t ctas = a.N <= 32u ? 2u : 1u;            // that fit an SM (registers, 96 or 128 KB of shared memory)
+    const uint32_t smem = (uint32_t)ssm_step_stages<LOG>() * SSM_STEP_THREADS * a.N * sizeof(float);
+    const uint32_t ctas = LOG <= 3 ? 2u : 1u;              // that fit an SM (registers, 96 or 128 KB of shared memory)
     const uint32_t rows = std::max<uint32_t>(1u, (uint32_t)c->n_sm * ctas / tiles);
-    launch_dep(kernel, dim3(tiles, std::min<uint32_t>(rows, a.S)), SSM_STEP_THREADS, smem, c->stream, a, log_lanes,
+    launch_dep(ssm_step_many_kernel<T, LOG>, dim3(tiles, std::min<uint32_t>(rows, a.S)), SSM_STEP_THREADS, smem, c->stream, a,
                static_cast<const float*>(c->ssm_ws.p));
     CU(cudaGetLastError());
     return SJA_OK;
@@ -1615,7 +1613,9 @@ sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
     // many jobs: persistent CTAs with the states streaming through shared memory
     if (vec && a.N <= 64u && (a.G << (log_lanes + 3u)) <= SSM_STEP_THREADS && a.D <= 65535u * SSM_STEP_THREADS &&
         (uint64_t)a.S * ((a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS) >= (uint64_t)SSM_STEP_MANY * c->n_sm)
-        return a.N <= 32u ? launch_ssm_step_many<T, 3>(c, a, log_lanes) : launch_ssm_step_many<T, 2>(c, a, log_lanes);
+        return log_lanes == 0u ? launch_ssm_step_many<T, 0>(c, a) : log_lanes == 1u ? launch_ssm_step_many<T, 1>(c, a)
+               : log_lanes == 2u ? launch_ssm_step_many<T, 2>(c, a) : log_lanes == 3u ? launch_ssm_step_many<T, 3>(c, a)
+                                                                                       : launch_ssm_step_many<T, 4>(c, a);
     const size_t smem = ((size_t)8u << log_lanes) * a.G * sizeof(float);
     // a job's channels are spread over up to eight CTAs (a portable cluster)
     const uint32_t ctas = std::min<uint32_t>(8u, (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS);

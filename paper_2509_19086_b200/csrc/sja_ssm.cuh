@@ -737,56 +737,86 @@ template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.
 
 // Then the states: a CTA keeps to 256 channels and goes from job to job, with the states of the next STAGES - 1 jobs on
 // their way into shared memory and the rows of the next one in registers, so that the memory never waits for a job's
-// arithmetic.
-template <typename T, int STAGES>
-__global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(const SsmArgs a, uint32_t log_lanes, const float* __restrict__ bc) {
+// arithmetic.  2^LOG lanes share a channel, four states each; up to 16 states A stays in registers.
+template <int LOG> __host__ __device__ constexpr int ssm_step_stages() { return LOG <= 3 ? 3 : 2; }
+template <typename T, int LOG>
+__global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(const SsmArgs a, const float* __restrict__ bc) {
+    constexpr uint32_t STAGES = ssm_step_stages<LOG>(), LANES = 1u << LOG, PASSES = LANES, PER = SSM_STEP_THREADS >> LOG;
+    constexpr bool KEEP_A = LOG <= 2;
     extern __shared__ __align__(16) float s_state[];        // [STAGES][256 channels][N]
-    __shared__ __align__(16) float s_bc[SSM_STEP_THREADS];  // B of group 0 .. G - 1, then C, each padded to 4 * lanes
+    __shared__ __align__(16) float s_bc[SSM_STEP_THREADS];  // B of group 0 .. G - 1, then C, each padded to 4 * LANES
     __shared__ float2 s_dd[SSM_STEP_THREADS];               // dt, dt u
     __shared__ float s_y[SSM_STEP_THREADS];
     dep_wait();
-    const uint32_t tid = threadIdx.x, lanes = 1u << log_lanes, base = blockIdx.x * SSM_STEP_THREADS, step = gridDim.y;
+    const uint32_t tid = threadIdx.x, base = blockIdx.x * SSM_STEP_THREADS, step = gridDim.y;
     const uint32_t here = min(a.D - base, SSM_STEP_THREADS), H = a.W > 1u ? a.W - 1u : 0u;
-    const uint32_t sub = tid & (lanes - 1u), n = sub * 4u, mine = tid >> log_lanes, per = SSM_STEP_THREADS >> log_lanes;
-    const uint32_t width = 2u * a.G << (log_lanes + 2u), to_C = width / 2u, stage = SSM_STEP_THREADS * a.N, hist_row = a.rows * (uint32_t)sizeof(T);
+    const uint32_t sub = tid % LANES, n = sub * 4u, mine = tid / LANES;
+    const uint32_t width = (2u * a.G) << (LOG + 2), to_C = width / 2u, stage = SSM_STEP_THREADS * a.N, hist_row = a.rows * (uint32_t)sizeof(T);
     const uint32_t c = base + min(tid, here - 1u);
+    // this thread's pieces: channels mine + p * PER of the tile, states n .. n + 3
+    const uint32_t el = mine * a.N + n, el_step = PER * a.N;
+    const uint32_t pieces = n >= a.N || mine >= here ? 0u : min(PASSES, (here - mine + PER - 1u) / PER);
     Conv cv;
     cv.load(a, c);
     const float skip = a.skip ? a.skip[c] : 0.0f, bias = a.dt_bias ? a.dt_bias[c] : 0.0f;
     const uint64_t DN = (uint64_t)a.D * a.N;
-    auto slot_at = [&](uint32_t s) { return s < a.S ? slot_of(a, s) : (int64_t)-1; };
-    // this thread's 16-byte pieces of the tile are the ones it works on later, so that it waits for its own only
-    auto start = [&](uint32_t to, int64_t slot) {
-        if (slot >= 0 && n < a.N)
-            for (uint32_t p = 0; p < lanes; ++p) {
-                const uint32_t local = p * per + mine;
-                if (local < here) copy_async16(s_state + to * stage + local * a.N + n, a.state + (uint64_t)slot * DN + (uint64_t)(base + local) * a.N + n);
-            }
+    const float* Ap = a.A + (uint64_t)base * a.N + el;
+    float4 A[KEEP_A ? PASSES : 1];
+    if (KEEP_A) {
+#pragma unroll
+        for (uint32_t p = 0; p < PASSES; ++p)
+            A[KEEP_A ? p : 0u] = p < pieces ? __ldg(reinterpret_cast<const float4*>(Ap + p * el_step)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    // where this thread's states of a job are (nullptr: not kept); pieces that it waits for are its own
+    auto states_of = [&](uint32_t s) -> float* {
+        const int64_t slot = s < a.S ? slot_of(a, s) : -1;
+        return slot >= 0 ? a.state + (uint64_t)slot * DN + (uint64_t)base * a.N + el : nullptr;
+    };
+    auto start = [&](uint32_t to, const float* from) {
+        float* dst = s_state + to * stage + el;
+        if (from) {
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; ++p)
+                if (p < pieces) copy_async16(dst + p * el_step, from + p * el_step);
+        }
         copy_commit();
     };
-    T xv, dv, zv, past[3];
+    const uint32_t s0 = blockIdx.y;
+    const T* px = static_cast<const T*>(a.xbc) + (int64_t)s0 * a.xbc_stride + c;
+    const T* pd = static_cast<const T*>(a.dt) + (int64_t)s0 * a.dt_stride + c;
+    const T* pz = a.z ? static_cast<const T*>(a.z) + (int64_t)s0 * a.z_stride + c : nullptr;
+    T* py = static_cast<T*>(a.y) + (int64_t)s0 * a.y_stride + c;
+    const float* pbc = bc + (uint64_t)s0 * width + tid;
+    T xv = from_f32<T>(0.0f), dv = xv, zv = xv, past[3] = {xv, xv, xv};
     float bcv = 0.0f;
     T* hist = nullptr;
-    auto fetch = [&](uint32_t s, int64_t slot) {
-        hist = H && a.history && slot >= 0 ? static_cast<T*>(a.history) + slot * (int64_t)H * a.rows + c : nullptr;
+    auto fetch = [&](uint32_t s) {                          // the rows of job s, where the pointers are
+        hist = nullptr;
         if (s >= a.S) return;
-        xv = static_cast<const T*>(a.xbc)[(int64_t)s * a.xbc_stride + c];
-        dv = static_cast<const T*>(a.dt)[(int64_t)s * a.dt_stride + c];
-        if (a.z) zv = static_cast<const T*>(a.z)[(int64_t)s * a.z_stride + c];
+        if (H && a.history) {
+            const int64_t slot = slot_of(a, s);
+            if (slot >= 0) hist = static_cast<T*>(a.history) + slot * (int64_t)H * a.rows + c;
+        }
+        xv = *px;
+        dv = *pd;
+        if (pz) zv = *pz;
 #pragma unroll
         for (uint32_t k = 0; k < 3u; ++k) past[k] = k < H && hist ? *row_at(hist, k, hist_row) : from_f32<T>(0.0f);
-        if (tid < width) bcv = bc[(uint64_t)s * width + tid];
+        if (tid < width) bcv = __ldg(pbc);
+        px = row_at(px, step, a.xbc_bytes);
+        pd = row_at(pd, step, a.dt_bytes);
+        if (pz) pz = row_at(pz, step, a.z_bytes);
+        pbc += step * width;
     };
-    uint32_t s = blockIdx.y;
-    int64_t slots[STAGES];                                  // of this job and the next ones
+    float* states[STAGES];                                  // of this job and the next ones
 #pragma unroll
-    for (uint32_t i = 0; i < (uint32_t)STAGES; ++i) slots[i] = slot_at(s + i * step);
+    for (uint32_t i = 0; i < STAGES; ++i) states[i] = states_of(s0 + i * step);
 #pragma unroll
-    for (uint32_t i = 0; i + 1u < (uint32_t)STAGES; ++i) start(i, slots[i]);
-    fetch(s, slots[0]);
+    for (uint32_t i = 0; i + 1u < STAGES; ++i) start(i, states[i]);
+    fetch(s0);
     uint32_t at = 0;
-    for (; s < a.S; s += step) {
-        start(at == 0u ? STAGES - 1u : at - 1u, slots[STAGES - 1]);     // its stage was emptied by the job before
+    for (uint32_t s = s0; s < a.S; s += step) {
+        start(at == 0u ? STAGES - 1u : at - 1u, states[STAGES - 1u]);      // its stage was emptied by the job before
         // convolution, time step and gate of one channel
         float gate = 1.0f;
         const float f0 = to_f32(past[0]), f1 = to_f32(past[1]), f2v = to_f32(past[2]);
@@ -800,42 +830,43 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
         s_dd[tid] = make_float2(dt, dt * u);
         if (a.z) gate = silu(to_f32(zv));
         if (tid < width) s_bc[tid] = bcv;
-        fetch(s + step, slots[1]);
+        fetch(s + step);
+        float* const next = states_of(s + STAGES * step);
         copy_wait<STAGES - 1>();
         __syncthreads();
-        const float* tile = s_state + at * stage;
-        float* state = slots[0] >= 0 ? a.state + (uint64_t)slots[0] * DN : nullptr;
+        const float* tile = s_state + at * stage + el;
         float4 B = *reinterpret_cast<const float4*>(s_bc + n), C = *reinterpret_cast<const float4*>(s_bc + n + to_C);
-#pragma unroll 4
-        for (uint32_t p = 0; p < lanes; ++p) {
-            const uint32_t local = p * per + mine;
-            const bool live = local < here && n < a.N;
-            const uint32_t el = live ? local * a.N + n : 0u;
+#pragma unroll
+        for (uint32_t p = 0; p < PASSES; ++p) {
+            const uint32_t local = p * PER + mine;
             const float2 dd = s_dd[local];
             if (a.G > 1u) {
-                const float* bq = s_bc + n + (((live ? base + local : 0u) / (a.D / a.G)) << (log_lanes + 2u));
+                const float* bq = s_bc + n + ((min(base + local, a.D - 1u) / (a.D / a.G)) << (LOG + 2));
                 B = *reinterpret_cast<const float4*>(bq);
                 C = *reinterpret_cast<const float4*>(bq + to_C);
             }
-            float4 h = state && live ? *reinterpret_cast<const float4*>(tile + el) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            const float4 A = __ldg(reinterpret_cast<const float4*>(a.A + (uint64_t)base * a.N + el));
+            float4 h = states[0] && p < pieces ? *reinterpret_cast<const float4*>(tile + p * el_step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float4 q = A[KEEP_A ? p : 0u];
+            if (!KEEP_A) q = p < pieces ? __ldg(reinterpret_cast<const float4*>(Ap + p * el_step)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             const float dl = dd.x * LOG2E;
-            h.x = fmaf(exp2_fast(dl * A.x), h.x, dd.y * B.x);
-            h.y = fmaf(exp2_fast(dl * A.y), h.y, dd.y * B.y);
-            h.z = fmaf(exp2_fast(dl * A.z), h.z, dd.y * B.z);
-            h.w = fmaf(exp2_fast(dl * A.w), h.w, dd.y * B.w);
+            h.x = fmaf(exp2_fast(dl * q.x), h.x, dd.y * B.x);
+            h.y = fmaf(exp2_fast(dl * q.y), h.y, dd.y * B.y);
+            h.z = fmaf(exp2_fast(dl * q.z), h.z, dd.y * B.z);
+            h.w = fmaf(exp2_fast(dl * q.w), h.w, dd.y * B.w);
             float acc = fmaf(h.x, C.x, h.y * C.y) + fmaf(h.z, C.z, h.w * C.w);
-            if (n >= a.N) acc = 0.0f;
-            for (uint32_t m = 1; m < lanes; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
+            if (p >= pieces) acc = 0.0f;
+#pragma unroll
+            for (uint32_t m = 1; m < LANES; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
             if (sub == 0u) s_y[local] = acc;
-            if (state && live) *reinterpret_cast<float4*>(state + (uint64_t)base * a.N + el) = h;
+            if (states[0] && p < pieces) *reinterpret_cast<float4*>(states[0] + p * el_step) = h;
         }
         __syncthreads();
-        if (tid < here) static_cast<T*>(a.y)[(int64_t)s * a.y_stride + c] = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
+        if (tid < here) *py = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
+        py = row_at(py, step, a.y_bytes);
 #pragma unroll
-        for (int i = 0; i + 1 < STAGES; ++i) slots[i] = slots[i + 1];
-        slots[STAGES - 1] = slot_at(s + STAGES * step);
-        at = at + 1u == (uint32_t)STAGES ? 0u : at + 1u;
+        for (uint32_t i = 0; i + 1u < STAGES; ++i) states[i] = states[i + 1u];
+        states[STAGES - 1u] = next;
+        at = at + 1u == STAGES ? 0u : at + 1u;
     }
     copy_wait<0>();
 }
