@@ -767,11 +767,12 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
         for (uint32_t p = 0; p < PASSES; ++p)
             A[KEEP_A ? p : 0u] = p < pieces ? __ldg(reinterpret_cast<const float4*>(Ap + p * el_step)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    // where this thread's states of a job are (nullptr: not kept); pieces that it waits for are its own
-    auto states_of = [&](uint32_t s) -> float* {
-        const int64_t slot = s < a.S ? slot_of(a, s) : -1;
-        return slot >= 0 ? a.state + (uint64_t)slot * DN + (uint64_t)base * a.N + el : nullptr;
+    // Slot numbers are read two jobs before anything depends on them.
+    auto slot_word = [&](uint32_t s) { return s >= a.S ? -1 : a.slots ? __ldg(a.slots + s) : (int32_t)s; };
+    auto states_of = [&](int32_t slot) -> float* {          // this thread's states of a job (nullptr: not kept)
+        return (uint32_t)slot < a.n_slots ? a.state + (uint64_t)slot * DN + (uint64_t)base * a.N + el : nullptr;
     };
+    // (the pieces that a thread waits for are its own)
     auto start = [&](uint32_t to, const float* from) {
         float* dst = s_state + to * stage + el;
         if (from) {
@@ -790,13 +791,11 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
     T xv = from_f32<T>(0.0f), dv = xv, zv = xv, past[3] = {xv, xv, xv};
     float bcv = 0.0f;
     T* hist = nullptr;
-    auto fetch = [&](uint32_t s) {                          // the rows of job s, where the pointers are
+    auto fetch = [&](uint32_t s, int32_t slot) {            // the rows of job s, where the pointers are
         hist = nullptr;
         if (s >= a.S) return;
-        if (H && a.history) {
-            const int64_t slot = slot_of(a, s);
-            if (slot >= 0) hist = static_cast<T*>(a.history) + slot * (int64_t)H * a.rows + c;
-        }
+        if (H && a.history && (uint32_t)slot < a.n_slots)
+            hist = static_cast<T*>(a.history) + (uint64_t)slot * H * a.rows + c;
         xv = *px;
         dv = *pd;
         if (pz) zv = *pz;
@@ -808,15 +807,15 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
         if (pz) pz = row_at(pz, step, a.z_bytes);
         pbc += step * width;
     };
-    float* states[STAGES];                                  // of this job and the next ones
+    int32_t slots[STAGES + 1];                              // of this job and the next ones
 #pragma unroll
-    for (uint32_t i = 0; i < STAGES; ++i) states[i] = states_of(s0 + i * step);
+    for (uint32_t i = 0; i <= STAGES; ++i) slots[i] = slot_word(s0 + i * step);
 #pragma unroll
-    for (uint32_t i = 0; i + 1u < STAGES; ++i) start(i, states[i]);
-    fetch(s0);
+    for (uint32_t i = 0; i + 1u < STAGES; ++i) start(i, states_of(slots[i]));
+    fetch(s0, slots[0]);
     uint32_t at = 0;
     for (uint32_t s = s0; s < a.S; s += step) {
-        start(at == 0u ? STAGES - 1u : at - 1u, states[STAGES - 1u]);      // its stage was emptied by the job before
+        start(at == 0u ? STAGES - 1u : at - 1u, states_of(slots[STAGES - 1u]));      // its stage was emptied by the job before
         // convolution, time step and gate of one channel
         float gate = 1.0f;
         const float f0 = to_f32(past[0]), f1 = to_f32(past[1]), f2v = to_f32(past[2]);
@@ -830,8 +829,11 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
         s_dd[tid] = make_float2(dt, dt * u);
         if (a.z) gate = silu(to_f32(zv));
         if (tid < width) s_bc[tid] = bcv;
-        fetch(s + step);
-        float* const next = states_of(s + STAGES * step);
+        fetch(s + step, slots[1]);
+        float* const state = states_of(slots[0]);
+#pragma unroll
+        for (uint32_t i = 0; i < STAGES; ++i) slots[i] = slots[i + 1u];
+        slots[STAGES] = slot_word(s + (STAGES + 1u) * step);
         copy_wait<STAGES - 1>();
         __syncthreads();
         const float* tile = s_state + at * stage + el;
@@ -845,7 +847,7 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
                 B = *reinterpret_cast<const float4*>(bq);
                 C = *reinterpret_cast<const float4*>(bq + to_C);
             }
-            float4 h = states[0] && p < pieces ? *reinterpret_cast<const float4*>(tile + p * el_step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float4 h = state && p < pieces ? *reinterpret_cast<const float4*>(tile + p * el_step) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             float4 q = A[KEEP_A ? p : 0u];
             if (!KEEP_A) q = p < pieces ? __ldg(reinterpret_cast<const float4*>(Ap + p * el_step)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             const float dl = dd.x * LOG2E;
@@ -858,14 +860,11 @@ __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(cons
 #pragma unroll
             for (uint32_t m = 1; m < LANES; m *= 2) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, m);
             if (sub == 0u) s_y[local] = acc;
-            if (states[0] && p < pieces) *reinterpret_cast<float4*>(states[0] + p * el_step) = h;
+            if (state && p < pieces) *reinterpret_cast<float4*>(state + p * el_step) = h;
         }
         __syncthreads();
         if (tid < here) *py = from_f32<T>(fmaf(skip, u, s_y[tid]) * gate);
         py = row_at(py, step, a.y_bytes);
-#pragma unroll
-        for (uint32_t i = 0; i + 1u < STAGES; ++i) states[i] = states[i + 1u];
-        states[STAGES - 1u] = next;
         at = at + 1u == STAGES ? 0u : at + 1u;
     }
     copy_wait<0>();
