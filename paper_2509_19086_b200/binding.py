@@ -174,7 +174,7 @@ class Sja:
         if st != SJA_OK:
             self._h = ctypes.c_void_p()
             raise SjaError(st, "sja_create failed (is a CUDA device present?)")
-        self.device, self.stream, self._torch_device = int(device), int(stream or 0), None
+        self.device, self.stream = int(device), int(stream or 0)
         self.n_jobs = 0
         self.n_gaps = 0
 
@@ -417,20 +417,22 @@ class Sja:
         descending order, ties to the lowest, and their ``top_logp`` f32 (R, top)."""
         torch = _torch()
         code = self._rows("logits", logits, None, None)
-        R, V = logits.shape
-        if tokens is not None:
+        R, V = logits.size(0), logits.size(1)
+        if tokens is not None and not (tokens.dtype is torch.int64 and tokens.is_cuda and tokens.get_device() == self.device and
+                                       tokens.dim() == 1 and tokens.size(0) == R and tokens.is_contiguous()):
             self._flat("tokens", tokens, torch.int64, (R,))
-        top = int(top)
         a = SjaTokenRows(code, top, R, V, scale, logits.data_ptr(), logits.stride(0) if R > 1 else V)
-        empty = self._allocator((logits, tokens))
-        entropy = empty((R,), torch.float32)
+        f32, empty = torch.float32, logits.new_empty
+        if torch._C._cuda_getCurrentRawStream(self.device) != self.stream:
+            empty = self._own_stream_empty(logits, (logits, tokens))
+        entropy = empty((R,), dtype=f32)
         a.entropy = entropy.data_ptr()
         out = {"entropy": entropy}
         if tokens is not None:
-            out["logp"] = logp = empty((R,), torch.float32)
+            out["logp"] = logp = empty((R,), dtype=f32)
             a.tokens, a.logp = tokens.data_ptr(), logp.data_ptr()
         if 0 <= top <= 32:
-            out["top_logp"], out["top_ids"] = top_logp, top_ids = empty((R, top), torch.float32), empty((R, top), torch.int32)
+            out["top_logp"], out["top_ids"] = top_logp, top_ids = empty((R, top), dtype=f32), empty((R, top), dtype=torch.int32)
             a.top_logp, a.top_ids = top_logp.data_ptr(), top_ids.data_ptr()
         st = self._lib.sja_token_stats(self._h, ctypes.byref(a))
         if st:
@@ -439,37 +441,31 @@ class Sja:
 
     def _rows(self, name, t, shape, dtype) -> int:
         """A CUDA tensor of rows (each contiguous) on this context's device; returns its sja_dtype."""
-        if not _is_torch(t):
-            raise TypeError(f"{name}: a tensor on CUDA device {self.device} is needed")
         _torch()
-        code = _DTYPE_CODES.get(t.dtype)
+        code = _DTYPE_CODES.get(getattr(t, "dtype", None))
         if code is None or not t.is_cuda or t.get_device() != self.device:
             raise TypeError(f"{name}: a float32, float16 or bfloat16 tensor on CUDA device {self.device} is needed")
-        if dtype is not None and t.dtype != dtype:
+        if dtype is not None and t.dtype is not dtype:
             raise TypeError(f"{name}: {t.dtype}, where the rows are {dtype}")
-        if t.dim() != 2 or (shape is not None and t.shape != shape):
+        if t.dim() != 2 or (shape is not None and (t.size(0) != shape[0] or t.size(1) != shape[1])):
             raise ValueError(f"{name}: shape {tuple(t.shape)}" + (f", not {shape}" if shape else " is not (rows, columns)"))
-        if t.stride(1) != 1 and t.shape[1] > 1:
+        if t.stride(1) != 1 and t.size(1) > 1:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
         return code
 
     def _flat(self, name, t, dtype, shape) -> None:
         """A contiguous CUDA tensor of one type and shape (None in the shape: any length)."""
-        if not _is_torch(t) or t.dtype != dtype or not t.is_cuda or t.get_device() != self.device:
+        if not _is_torch(t) or t.dtype is not dtype or not t.is_cuda or t.get_device() != self.device:
             raise TypeError(f"{name}: a {dtype} tensor on CUDA device {self.device} is needed")
-        if t.shape != shape and (t.dim() != len(shape) or any(w is not None and v != w for v, w in zip(t.shape, shape))):
+        if t.dim() != len(shape) or any(w is not None and v != w for v, w in zip(t.shape, shape)):
             raise ValueError(f"{name}: shape {tuple(t.shape)}, not {shape}")
         if not t.is_contiguous():
             raise ValueError(f"{name}: must be contiguous")
 
-    def _allocator(self, used):
-        """What makes the tensors for a call's results.  Where torch works on another stream than the context, their
+    def _own_stream_empty(self, like, used):
+        """What makes the tensors for a call's results where torch works on another stream than the context: their
         memory belongs to the context's stream, and the tensors the call uses are kept until that stream is through."""
         torch = _torch()
-        if self._torch_device is None:
-            self._torch_device = torch.device("cuda", self.device)
-        if torch._C._cuda_getCurrentRawStream(self.device) == self.stream:
-            return lambda shape, dtype: torch.empty(shape, dtype=dtype, device=self._torch_device)
         mine = torch.cuda.ExternalStream(self.stream, device=self.device)
         for t in used:
             if t is not None:
@@ -477,7 +473,7 @@ class Sja:
 
         def empty(shape, dtype):
             with torch.cuda.stream(mine):
-                return torch.empty(shape, dtype=dtype, device=self._torch_device)
+                return like.new_empty(shape, dtype=dtype)
         return empty
 
     # -- sja_debug_fail_alloc
@@ -526,14 +522,15 @@ class SsmLayer:
                             skip=ptr[3], dt_bias=ptr[4])
 
     def _fill(self, xbc, dt, z, state, history, slots, n_jobs, out, more=()):
-        """Check one call's tensors and write them into the call's arguments; returns (arguments, y)."""
-        ctx, torch = self.ctx, _torch()
+        """Check one call's tensors and write them into the call's arguments; returns (arguments, y).  The checks are
+        spelled out: a call for a few tokens lasts about as long as they do."""
+        ctx, torch, D, dev = self.ctx, _torch(), self.D, self.ctx.device
         a = SjaSsm.from_buffer_copy(self._args)
         a.dtype = ctx._rows("xbc", xbc, None, None)
-        T, row_type = xbc.shape[0], xbc.dtype
-        if xbc.shape[1] != self.rows:
-            raise ValueError(f"xbc: rows of {xbc.shape[1]}, not D + 2GN = {self.rows}")
-        shape = (T, self.D)
+        T, row_type = xbc.size(0), xbc.dtype
+        if xbc.size(1) != self.rows:
+            raise ValueError(f"xbc: rows of {xbc.size(1)}, not D + 2GN = {self.rows}")
+        shape = (T, D)
         ctx._rows("dt", dt, shape, row_type)
         a.xbc, a.dt = xbc.data_ptr(), dt.data_ptr()
         if z is not None:
@@ -541,41 +538,55 @@ class SsmLayer:
             a.z = z.data_ptr()
         n_slots = n_jobs
         if state is not None:
-            ctx._flat("state", state, torch.float32, (None, self.D, self.N))
-            n_slots = state.shape[0]
+            if not (state.dtype is torch.float32 and state.is_cuda and state.get_device() == dev and state.dim() == 3 and
+                    state.size(1) == D and state.size(2) == self.N and state.is_contiguous()):
+                ctx._flat("state", state, torch.float32, (None, D, self.N))
+            n_slots = state.size(0)
             a.state = state.data_ptr()
         if history is not None:
-            ctx._flat("history", history, row_type, (None if state is None else n_slots, max(self.W - 1, 0), self.rows))
-            n_slots = history.shape[0]
-            if self.W > 1:
+            keep = self.W - 1 if self.W > 1 else 0
+            if not (history.dtype is row_type and history.is_cuda and history.get_device() == dev and history.dim() == 3 and
+                    history.size(1) == keep and history.size(2) == self.rows and history.is_contiguous() and
+                    (state is None or history.size(0) == n_slots)):
+                ctx._flat("history", history, row_type, (None if state is None else n_slots, keep, self.rows))
+            n_slots = history.size(0)
+            if keep:
                 a.history = history.data_ptr()
         a.n_slots = n_slots
         if slots is not None:
-            ctx._flat("slots", slots, torch.int32, (n_jobs,))
+            if not (slots.dtype is torch.int32 and slots.is_cuda and slots.get_device() == dev and slots.dim() == 1 and
+                    slots.size(0) == n_jobs and slots.is_contiguous()):
+                ctx._flat("slots", slots, torch.int32, (n_jobs,))
             a.slots = slots.data_ptr()
-        if out is None:
-            out = ctx._allocator((xbc, dt, z, state, history, slots) + more)(shape, row_type)
-        else:
+        same = torch._C._cuda_getCurrentRawStream(dev) == ctx.stream
+        if out is not None:
             ctx._rows("out", out, shape, row_type)
+        elif same:
+            out = xbc.new_empty(shape)
+        if not same:
+            empty = ctx._own_stream_empty(xbc, (xbc, dt, z, state, history, slots, out) + more)
+            out = empty(shape, row_type) if out is None else out
         a.y = out.data_ptr()
         if T > 1:
             a.xbc_stride, a.dt_stride, a.y_stride = xbc.stride(0), dt.stride(0), out.stride(0)
             if z is not None:
                 a.z_stride = z.stride(0)
         else:                                           # the stride of a single row says nothing
-            a.xbc_stride, a.dt_stride, a.z_stride, a.y_stride = self.rows, self.D, self.D, self.D
+            a.xbc_stride, a.dt_stride, a.z_stride, a.y_stride = self.rows, D, D, D
         return a, out
 
     def prompt(self, xbc, dt, off, state=None, history=None, z=None, slots=None, resume: bool = False, out=None):
         """sja_ssm_prompt: the packed tokens of S jobs, job s at rows ``off[s]`` .. ``off[s + 1] - 1`` (``off`` int64
         (S + 1,) on the device).  ``resume``: go on from the slots instead of from zero.  Returns y (T, D)."""
         ctx = self.ctx
-        ctx._flat("off", off, _torch().int64, (None,))
-        S = off.shape[0] - 1
+        if not (getattr(off, "dtype", None) is _torch().int64 and off.is_cuda and off.get_device() == ctx.device and off.dim() == 1 and
+                off.is_contiguous()):
+            ctx._flat("off", off, _torch().int64, (None,))
+        S = off.size(0) - 1
         if S < 0:
             raise ValueError("off: needs one entry per job and one more")
         a, y = self._fill(xbc, dt, z, state, history, slots, S, out, (off,))
-        st = ctx._lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), S, xbc.shape[0], off.data_ptr(), 1 if resume else 0)
+        st = ctx._lib.sja_ssm_prompt(ctx._h, ctypes.byref(a), S, xbc.size(0), off.data_ptr(), 1 if resume else 0)
         if st:
             ctx._check(st)
         return y
@@ -583,8 +594,9 @@ class SsmLayer:
     def step(self, xbc, dt, state, history=None, z=None, slots=None, out=None):
         """sja_ssm_step: one token for each of S jobs, continued from and kept in their slots.  Returns y (S, D)."""
         ctx = self.ctx
-        a, y = self._fill(xbc, dt, z, state, history, slots, xbc.shape[0], out)
-        st = ctx._lib.sja_ssm_step(ctx._h, ctypes.byref(a), xbc.shape[0])
+        S = xbc.size(0)
+        a, y = self._fill(xbc, dt, z, state, history, slots, S, out)
+        st = ctx._lib.sja_ssm_step(ctx._h, ctypes.byref(a), S)
         if st:
             ctx._check(st)
         return y

@@ -527,8 +527,9 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
         if (lane == 0u) s_max[warp] = bound;
     }
     __syncthreads();
-    all = s_stat[0];
-    for (int w = 1; w < WARPS; ++w) all = stat_join(all, s_stat[w], a.c);
+    all = s_stat[lane % WARPS];
+#pragma unroll
+    for (uint32_t m = WARPS / 2; m; m >>= 1) all = stat_join(all, stat_shuffle(all, m), a.c);
     RowStat rs;
     if (n_rank == 1u) {
         rs = RowStat(all, a.c);
@@ -640,8 +641,8 @@ __global__ void __launch_bounds__(THREADS) token_stats_kernel(const TokenArgs a)
     asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (rank) return;
-    all = s_part[0];
-    for (uint32_t w = 1; w < n_rank; ++w) all = stat_join(all, s_part[w], a.c);
+    all = s_part[lane % n_rank];                                     // (a power of two)
+    for (uint32_t m = n_rank / 2u; m; m >>= 1) all = stat_join(all, stat_shuffle(all, m), a.c);
     rs = RowStat(all, a.c);
     if (tid == 0u) token.put(a, r, rs);
     const uint32_t want = min(a.top, a.V);
