@@ -1,0 +1,71 @@
+"""A scheduling round on forecast envelopes: the observed first half of every job's memory trace goes through a small
+sequence model, which then predicts the envelope of the second half step by step; the jobs are loaded at their progress
+points with the predicted values, and one round is run.
+
+    python examples/forecast_round.py
+
+The model's weights are random, so its forecasts are cautious rather than good: what is shown is how the calls follow
+one another.
+"""
+import os
+import sys
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2509_19086_b200 import binding, forecast  # noqa: E402
+from paper_2509_19086_b200 import workloads as wl  # noqa: E402
+
+
+def forecast_profiles(ctx, prof, bins, eps=0.1, top=32, seed=0):
+    """Profiles whose second halves carry forecast envelopes, the progress points, and how the first halves fared:
+    mean negative log likelihood and entropy of the model's answers."""
+    lens = np.diff(prof.off).astype(np.int64)
+    seen = lens // 2
+    rows = np.concatenate([np.arange(o, o + n) for o, n in zip(prof.off[:-1].astype(np.int64), seen)])
+    off = torch.tensor(np.concatenate([[0], np.cumsum(seen)]), device="cuda")
+    tokens = bins.tokens(torch.tensor(prof.mem_MiB[rows].astype(np.int64), device="cuda"))
+    model = forecast.Forecaster(ctx, bins.n_bins, prof.n_jobs, seed=seed)
+
+    logits = model.observe(tokens, off)
+    # each token was answered by the row before it; a job's first token is not scored
+    given = torch.cat([tokens[1:], tokens[:1]])
+    given[off[1:] - 1] = -1
+    stats = ctx.token_stats(logits, given)
+    scored = (given >= 0).sum()
+    nll, entropy = -stats["logp"].sum() / scored, stats["entropy"].mean()
+
+    mem = prof.mem_MiB.copy()
+    last = logits[off[1:] - 1]
+    begin = torch.tensor(prof.off[:-1].astype(np.int64) + seen, device="cuda")
+    left = torch.tensor(lens - seen, device="cuda")
+    values = torch.empty(int(prof.n_steps), dtype=torch.int64, device="cuda")
+    values.fill_(-1)
+    for i in range(int((lens - seen).max())):
+        answer = ctx.token_stats(last, top=top)
+        upper = forecast.envelope(answer["top_logp"], answer["top_ids"], eps, bins.n_bins)
+        running = i < left
+        values[(begin + i)[running]] = bins.upper_MiB(upper)[running]
+        last = model.advance(answer["top_ids"][:, 0].long())
+    got = values.cpu().numpy()
+    mem[got >= 0] = got[got >= 0].astype(np.uint32)
+    return wl.Profiles(prof.off, prof.dur_ms, mem, prof.safe_bits, prof.ready_ms, prof.wait_ms, prof.prio), seen.astype(np.uint32), float(nll), float(entropy)
+
+
+def main(n_jobs=64, steps=256, n_gaps=16):
+    spec = wl.scaled(wl.SPECS[0], n_jobs=n_jobs, fixed_len=steps, n_gaps=n_gaps)
+    prof, gaps, bins = wl.make_profiles(spec, threads=1), wl.make_gaps(spec), forecast.MemoryBins(256)
+    with binding.Sja() as ctx:
+        predicted, progress, nll, entropy = forecast_profiles(ctx, prof, bins)
+        ctx.load_profiles(predicted.off, predicted.dur_ms, predicted.mem_MiB, predicted.safe_bits, predicted.ready_ms, progress=progress)
+        ctx.advertise(gaps)
+        awards = ctx.select(spec.policy, out="host")
+        granted = ctx.commit()
+    print(f"{n_jobs} jobs, {int(progress.sum())} observed steps: {nll:.2f} nats a step against an entropy of {entropy:.2f}; "
+          f"{granted} of {n_gaps} gaps granted on the forecast envelopes")
+    return predicted, progress, gaps, awards, spec
+
+
+if __name__ == "__main__":
+    main()

@@ -93,7 +93,7 @@ struct RowStat {
     __device__ __forceinline__ RowStat(const Stat& t, float c) {
         const bool empty = t.m == -INFINITY && t.s == 0.0f;      // nothing but -inf
         m = empty ? 0.0f : t.m;
-        log_s = empty ? 0.0f : __log2f(t.s);
+        log_s = empty ? 0.0f : log2f(t.s);          // (the fast one loses half of its bits next to 1)
         entropy = empty ? 0.0f : LN2 * (log_s - t.w / t.s);
         if (scaled_fits(m, c)) log_s -= fmaf(m, c, -(m * c));
     }

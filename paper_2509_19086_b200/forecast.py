@@ -1,0 +1,94 @@
+"""A small sequence model of job profiles, from the library's scan and token statistics (sja_ssm_prompt, sja_ssm_step,
+sja_token_stats): what stands between the telemetry of running jobs and the envelopes a scheduling round works on.
+
+The paper leaves the predictive layer to further work (Section 5.3); it asks of it, per step, a risk-adjusted envelope
+U(t) = Q_{1-eps}[M(t)] (Section 3.9), refined as predictions improve.  Here a job's memory values are tokens
+(:class:`MemoryBins`), a :class:`Forecaster` keeps a recurrent state per job slot -- its history goes through once, as a
+prompt, each further step as a single token -- and :func:`envelope` reads U off the likeliest bins.  Matrix products are
+torch's; the weights are the caller's (``Forecaster`` draws random ones, which forecast nothing).
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import binding
+
+
+class MemoryBins:
+    """Memory values in MiB as tokens: bin b holds the values up to ``edge(b)``, edges spaced evenly in the logarithm."""
+
+    def __init__(self, n_bins: int, lo_MiB: float = 64.0, hi_MiB: float = 81920.0):
+        if n_bins < 2 or not 0 < lo_MiB < hi_MiB:
+            raise ValueError("MemoryBins: at least two bins, 0 < lo < hi")
+        self.n_bins = n_bins
+        self.edges = torch.tensor([math.ceil(lo_MiB * (hi_MiB / lo_MiB) ** (b / (n_bins - 1))) for b in range(n_bins)], dtype=torch.int64)
+
+    def tokens(self, mem_MiB: torch.Tensor) -> torch.Tensor:
+        """The lowest bin whose edge is not below the value (the last bin for larger ones)."""
+        return torch.bucketize(mem_MiB.to(torch.int64), self.edges.to(mem_MiB.device)).clamp(max=self.n_bins - 1)
+
+    def upper_MiB(self, tokens: torch.Tensor) -> torch.Tensor:
+        """The largest memory value of each token's bin."""
+        return self.edges.to(tokens.device)[tokens.long()]
+
+
+def envelope(top_logp: torch.Tensor, top_ids: torch.Tensor, eps: float, n_bins: int) -> torch.Tensor:
+    """Bin that holds Q_{1-eps} of each row, from its alternatives (R, k) in descending order: the largest bin of the
+    smallest set of alternatives that holds 1 - eps of the probability, so that P(M <= U) >= 1 - eps.  Where the
+    alternatives hold less than that, the last bin."""
+    p = torch.exp(top_logp)
+    mass = p.cumsum(dim=1)
+    needed = mass - p < 1.0 - eps
+    largest = torch.where(needed, top_ids, torch.zeros_like(top_ids)).max(dim=1).values
+    return torch.where(mass[:, -1] >= 1.0 - eps, largest, torch.full_like(largest, n_bins - 1))
+
+
+class Forecaster:
+    """``n_layers`` layers of scan and gate over ``width`` channels, one state slot per job.
+
+    ``observe`` takes the packed histories of jobs (tokens, CSR offsets, slots), ``advance`` one further token of each;
+    both return logits over the bins of the step that follows each token."""
+
+    def __init__(self, ctx: "binding.Sja", n_bins: int, n_jobs: int, width: int = 128, n_layers: int = 2, n_state: int = 16,
+                 conv_width: int = 4, dtype=torch.bfloat16, seed: int = 0):
+        dev = torch.device("cuda", ctx.device)
+        g = torch.Generator(device=dev)
+        g.manual_seed(seed)
+        rn = lambda *s: torch.randn(*s, device=dev, generator=g)
+        self.n_bins, self.width, self.rows, self.dtype = n_bins, width, width + 2 * n_state, dtype
+        self.embedding = rn(n_bins, width).to(dtype)
+        self.layers = []
+        for _ in range(n_layers):
+            scan = ctx.ssm_layer(-torch.arange(1, n_state + 1, device=dev, dtype=torch.float32).repeat(width, 1).contiguous(),
+                                 conv_w=rn(self.rows, conv_width) / math.sqrt(conv_width), conv_b=torch.zeros(self.rows, device=dev),
+                                 skip=torch.ones(width, device=dev), dt_bias=rn(width) - 4.0)
+            self.layers.append({
+                "scan": scan,
+                "into": (rn(width, self.rows + 2 * width) / math.sqrt(width)).to(dtype),     # row | time step | gate
+                "out": (rn(width, width) / math.sqrt(width)).to(dtype),
+                "state": torch.zeros(n_jobs, width, n_state, device=dev),
+                "history": torch.zeros(n_jobs, conv_width - 1, self.rows, device=dev, dtype=dtype)})
+
+    @staticmethod
+    def _norm(x):
+        f = x.float()
+        return (f * torch.rsqrt(f.square().mean(dim=1, keepdim=True) + 1e-6)).to(x.dtype)
+
+    def _run(self, tokens, scan):
+        x = self.embedding[tokens]
+        for layer in self.layers:
+            rows = self._norm(x) @ layer["into"]
+            r, w = self.rows, self.width
+            x = x + scan(layer, rows[:, :r], rows[:, r:r + w], rows[:, r + w:]) @ layer["out"]
+        return self._norm(x) @ (self.embedding.t() / math.sqrt(self.width))
+
+    def observe(self, tokens, off, slots=None, resume: bool = False):
+        """Histories: ``tokens`` (T,) of all jobs one after another, ``off`` int64 (S + 1,), ``slots`` int32 (S,)."""
+        return self._run(tokens, lambda l, xbc, dt, z: l["scan"].prompt(xbc, dt, off, state=l["state"], history=l["history"], z=z,
+                                                                         slots=slots, resume=resume))
+
+    def advance(self, tokens, slots=None):
+        """One further step: ``tokens`` (S,), one per job."""
+        return self._run(tokens, lambda l, xbc, dt, z: l["scan"].step(xbc, dt, l["state"], history=l["history"], z=z, slots=slots))

@@ -1,0 +1,51 @@
+"""The forecasting example end to end: prompts, single tokens and token statistics feeding a scheduling round."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def test_forecast_round_matches_the_oracle(oracle_mod):
+    from examples import forecast_round
+    predicted, progress, gaps, awards, spec = forecast_round.main(n_jobs=24, steps=40, n_gaps=12)
+    want = oracle_mod.select(predicted, progress, predicted.ready_ms.copy(), gaps, spec.policy)
+    for f in ("job", "end_step", "dur_ms", "score"):
+        assert np.array_equal(awards[f], want[f]), f
+    lens = np.diff(predicted.off).astype(np.int64)
+    assert (progress == lens // 2).all() and predicted.mem_MiB.min() >= 1 and predicted.mem_MiB.max() <= 81920
+
+
+def test_a_history_in_one_call_and_in_steps_gives_the_same_forecast():
+    import torch
+    from paper_2509_19086_b200 import binding, forecast
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    tokens = torch.randint(0, 64, (3, 50), device="cuda", generator=g)
+    slots = torch.tensor([4, 0, 2], device="cuda", dtype=torch.int32)
+    with binding.Sja() as ctx:
+        off = torch.tensor([0, 50, 100, 150], device="cuda")
+        whole = forecast.Forecaster(ctx, 64, 5, width=64, dtype=torch.float32).observe(tokens.reshape(-1), off, slots)[off[1:] - 1]
+        model = forecast.Forecaster(ctx, 64, 5, width=64, dtype=torch.float32)
+        model.observe(tokens[:, :20].reshape(-1), torch.tensor([0, 20, 40, 60], device="cuda"), slots)
+        model.observe(tokens[:, 20:40].reshape(-1), torch.tensor([0, 20, 40, 60], device="cuda"), slots, resume=True)
+        for t in range(40, 50):
+            last = model.advance(tokens[:, t], slots)
+    # two layers of 32-bit products over up to 96 values, twice in another order: a few hundred roundings of values of size 10
+    assert (last - whole).abs().max() <= 1e-3
+
+
+def test_envelope_holds_the_asked_for_mass():
+    import torch
+    from paper_2509_19086_b200 import binding, forecast
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    logits = torch.randn(500, 64, device="cuda", generator=g) * 3
+    with binding.Sja() as ctx:
+        a = ctx.token_stats(logits, top=32)
+    p = torch.softmax(logits.double(), dim=1)
+    for eps in (0.5, 0.1, 0.01):
+        u = forecast.envelope(a["top_logp"], a["top_ids"], eps, 64).long()
+        mass = p.cumsum(dim=1).gather(1, u[:, None])[:, 0]
+        assert (mass >= 1 - eps - 1e-5).all()
+        # the smallest set of alternatives, not all bins
+        assert eps < 0.5 or (u < 63).any()
