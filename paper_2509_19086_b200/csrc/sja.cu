@@ -1543,8 +1543,8 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
 #ifndef SSM_FEW
 #define SSM_FEW 65536u
 #endif
-#ifndef SSM_ONE_SEG
-#define SSM_ONE_SEG 128u
+#ifndef SSM_BY_JOB
+#define SSM_BY_JOB 256u
 #endif
 template <typename T>
 sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
@@ -1555,19 +1555,22 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         const uint32_t Dg = a.D / a.G, unit = 32u / sh.lanes;          // channels of a warp
         const uint32_t need = (Dg + unit - 1u) / unit;                 // warps of one group's channels
         // the widest CTA that leaves the fewest warps without a channel (they share the tile of B and C)
-        uint32_t warps = few ? 1u : SSM_THREADS / 32u;
+        uint32_t warps = few ? 4u : SSM_THREADS / 32u;
         while (warps > 1u && (need + warps - 1u) / warps * warps > (need + warps / 2u - 1u) / (warps / 2u) * (warps / 2u)) warps /= 2u;
         const uint32_t tiles = (need + warps - 1u) / warps * a.G;
         const uint64_t all = (uint64_t)need * a.G;
         uint64_t n_seg = std::max<uint64_t>(1, (uint64_t)c->n_sm * SSM_WARPS_PER_SM / all);
         n_seg = std::min<uint64_t>(n_seg, (a.T + 31u) / 32u);
-        if (a.T <= SSM_ONE_SEG || (n_seg < 3u && a.S == 1u)) n_seg = 1u;   // (two passes over half the tokens gain nothing)
+        if (n_seg < 3u && a.S == 1u) n_seg = 1u;                       // (two passes over half the tokens gain nothing)
         // about as many segments as jobs: then one each, which jobs of one length need not be cut for
         if (a.S > 1u && 3ull * a.S >= 2u * n_seg && a.S <= 2u * n_seg) n_seg = a.S;
+        // a short prompt is not cut: a CTA per job, and nothing to hand on
+        a.by_job = a.T <= SSM_BY_JOB && a.S <= 65535u ? 1u : 0u;
+        if (a.by_job) n_seg = a.S;
         n_seg = std::min<uint64_t>(n_seg, 65535u);
         a.seg_len = (a.T + n_seg - 1u) / n_seg;
-        a.n_seg = (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
-        if (a.n_seg > 1u) {
+        a.n_seg = a.by_job ? a.S : (uint32_t)((a.T + a.seg_len - 1u) / a.seg_len);
+        if (a.n_seg > 1u && !a.by_job) {
             const size_t DN = (size_t)a.D * a.N, n = a.n_seg;
             const size_t h = n * DN * 4u, f = a.resume && a.state ? h : 0u, s = n * a.D * 4u;
             TRY(reserve(c, c->ssm_ws, h + f + s + n * 4u));

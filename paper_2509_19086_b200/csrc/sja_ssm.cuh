@@ -33,7 +33,7 @@ struct SsmArgs {
     uint64_t T;
     uint32_t S, n_slots, D, N, G, W, rows, resume;
     // split of the token axis (prompts)
-    uint32_t n_seg;
+    uint32_t n_seg, by_job;       // by_job: segment k is job k
     uint64_t seg_len;
     uint32_t* seg_flag;           // [n_seg]
     float *seg_h, *seg_first, *seg_sdt;   // [n_seg, D, N], [n_seg, D, N], [n_seg, D]
@@ -125,6 +125,7 @@ __device__ __forceinline__ uint32_t warp_lower_bound(const uint64_t* __restrict_
 __device__ __forceinline__ uint64_t segment_bound(const SsmArgs& a, uint32_t k) {
     if (k == 0u) return 0ull;
     if (k >= a.n_seg) return a.T;
+    if (a.by_job) return a.off[k] < a.T ? a.off[k] : a.T;
     const uint64_t at = (uint64_t)k * a.seg_len;
     const uint32_t j = warp_lower_bound(a.off, a.S + 1u, at);
     if (j == 0u || j > a.S) return at < a.T ? at : a.T;
@@ -201,10 +202,7 @@ template <int K> __device__ __forceinline__ void load_pairs(F2 (&to)[K / 2], con
     }
 }
 
-#ifndef SSM_CTA
-#define SSM_CTA 256
-#endif
-constexpr uint32_t SSM_THREADS = SSM_CTA;    // most threads of a prompt CTA
+constexpr uint32_t SSM_THREADS = 256;    // most threads of a prompt CTA
 // Tokens whose B and C one CTA keeps at a time: a thread convolves a stretch of 8 tokens of one column (2 NP of them).
 __host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np <= 64u ? 1024u / np : 16u; }
 
@@ -216,10 +214,10 @@ __host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np 
 // CARRY = true is the first pass of a split: what the job that crosses the segment's end adds to its state inside the
 // segment, and its sum of time steps (exp(A sum dt) is the decay over the segment).
 template <typename T, int K, int LPC, bool CARRY>
-__global__ void __launch_bounds__(SSM_THREADS, (LPC > 1 && K <= 8 ? 3 : 2) * 256 / SSM_THREADS) ssm_prompt_kernel(const SsmArgs a) {
+__global__ void __launch_bounds__(SSM_THREADS, LPC > 1 && K <= 8 ? 3 : 2) ssm_prompt_kernel(const SsmArgs a) {
     constexpr uint32_t NP = K * LPC, TT = ssm_tile_tokens(NP), CPW = 32 / LPC, COLS = CARRY ? NP : 2 * NP;
     constexpr int U = 4, TPL = U / LPC, P = LPC, STRETCH = 8;
-    static_assert(LPC == 1 || LPC == 2 || LPC == 4, "four, two or one tokens a lane");
+    static_assert(LPC == 1 || LPC == 4, "four tokens a lane, or one");
     __shared__ __align__(16) float s_bc[2][TT * 2 * NP];       // [buffer][token][B | C]
     dep_wait();
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, sub = lane % LPC;
@@ -404,12 +402,8 @@ __global__ void __launch_bounds__(SSM_THREADS, (LPC > 1 && K <= 8 ? 3 : 2) * 256
                     b1v = __shfl_sync(0xFFFFFFFFu, sub < 3u ? cur[0] : prev[0], (sub + 3u) % 4u, 4);
                     b2v = __shfl_sync(0xFFFFFFFFu, sub < 2u ? cur[0] : prev[0], (sub + 2u) % 4u, 4);
                     b3v = __shfl_sync(0xFFFFFFFFu, sub < 1u ? cur[0] : prev[0], (sub + 1u) % 4u, 4);
-                } else if constexpr (LPC == 1) {
-                    b1v = prev[TPL - 1]; b2v = prev[TPL - 2]; b3v = prev[TPL - 3];
                 } else {
-                    b1v = __shfl_xor_sync(0xFFFFFFFFu, sub == 0u ? cur[TPL - 1] : prev[TPL - 1], 1);
-                    b2v = __shfl_xor_sync(0xFFFFFFFFu, sub == 0u ? cur[0] : prev[0], 1);
-                    b3v = prev[TPL - 1];
+                    b1v = prev[TPL - 1]; b2v = prev[TPL - 2]; b3v = prev[TPL - 3];
                 }
 #pragma unroll
                 for (int i = 0; i < TPL; ++i) {
@@ -459,11 +453,6 @@ __global__ void __launch_bounds__(SSM_THREADS, (LPC > 1 && K <= 8 ? 3 : 2) * 256
                         k1 += __shfl_xor_sync(0xFFFFFFFFu, high ? sum[1] : sum[3], 2);
                         const bool odd = sub & 1u;
                         sum[0] = (odd ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, odd ? k0 : k1, 1);
-                    } else if constexpr (LPC == 2) {
-                        const bool odd = sub & 1u;
-                        const float k0 = (odd ? sum[2] : sum[0]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? sum[0] : sum[2], 1);
-                        const float k1 = (odd ? sum[3] : sum[1]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? sum[1] : sum[3], 1);
-                        sum[0] = k0; sum[1] = k1;
                     }
 #pragma unroll
                     for (int i = 0; i < TPL; ++i)
@@ -502,15 +491,25 @@ __global__ void __launch_bounds__(256) ssm_carry_kernel(const SsmArgs a) {
     const uint64_t DN = (uint64_t)a.D * a.N, i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i >= DN) return;
     const uint32_t d = (uint32_t)(i / a.N);
-    const float A2 = a.A[i] * 1.44269504f;
+    const float A2 = a.A[i] * LOG2E;
     float carry = 0.0f;
-#pragma unroll 4
-    for (uint32_t k = 0; k + 1u < a.n_seg; ++k) {
-        const uint32_t flag = a.seg_flag[k];
-        if (flag == SEG_NONE) continue;
-        const float own = a.seg_h[k * DN + i];
-        carry = flag == SEG_STARTS ? own : fmaf(exp2_fast(A2 * a.seg_sdt[(uint64_t)k * a.D + d]), carry, own);
-        a.seg_h[k * DN + i] = carry;
+    constexpr uint32_t AHEAD = 8;                           // segments whose values are on their way together
+    for (uint32_t k0 = 0; k0 + 1u < a.n_seg; k0 += AHEAD) {
+        uint32_t flag[AHEAD];
+        float own[AHEAD], dt[AHEAD];
+#pragma unroll
+        for (uint32_t j = 0; j < AHEAD; ++j) {
+            const uint32_t k = min(k0 + j, a.n_seg - 2u);
+            flag[j] = k0 + j + 1u < a.n_seg ? a.seg_flag[k] : (uint32_t)SEG_NONE;
+            own[j] = a.seg_h[k * DN + i];                   // (of a segment that hands nothing on: not used)
+            dt[j] = a.seg_sdt[(uint64_t)k * a.D + d];
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < AHEAD; ++j) {
+            if (flag[j] == SEG_NONE) continue;
+            carry = flag[j] == SEG_STARTS ? own[j] : fmaf(exp2_fast(A2 * dt[j]), carry, own[j]);
+            a.seg_h[(k0 + j) * DN + i] = carry;
+        }
     }
 }
 
