@@ -85,6 +85,14 @@ SHAPES = [
     ([97, 200], 18, 100, 1, 4),
     ([260, 40], 9, 128, 1, 3),
     ([50, 20], 600, 16, 4, 4),
+    # more than 256 tokens are cut into segments; more than 65 536 values take the form for many channels
+    ([400, 0, 300, 1, 90], 128, 8, 1, 4),
+    ([1000], 90, 5, 3, 2),
+    ([70] * 12, 130, 16, 1, 0),
+    ([0, 500, 0, 0, 600, 0], 300, 16, 2, 4),
+    ([300, 280], 40, 31, 1, 4),
+    ([350, 17, 0], 24, 128, 1, 3),
+    ([600], 301, 13, 1, 1),
 ]
 
 

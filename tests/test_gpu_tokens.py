@@ -15,10 +15,12 @@ def ctx():
         yield c
 
 
-def _check(ctx, logits, tokens, top, scale=1.0):
+def _check(ctx, logits, tokens, top, scale=1.0, wait=lambda: None):
     import torch
     tok = torch.as_tensor(np.asarray(tokens, dtype=np.int64), device="cuda")
-    got = {k: v.cpu().numpy() for k, v in ctx.token_stats(logits, tok, top=top, scale=scale).items()}
+    out = ctx.token_stats(logits, tok, top=top, scale=scale)
+    wait()
+    got = {k: v.cpu().numpy() for k, v in out.items()}
     logp, entropy, top_logp, top_ids, bound = ref.token_stats(logits.double().cpu().numpy(), tokens, top, scale)
     assert np.array_equal(got["top_ids"], top_ids)
     for name, want, b in (("logp", logp, bound), ("entropy", entropy, bound), ("top_logp", top_logp, bound[:, None])):
@@ -97,6 +99,16 @@ def test_tokens_outside_the_row_and_single_outputs(ctx):
     assert "logp" not in out and out["top_ids"].shape == (4, 3)
     assert torch.equal(out["top_ids"][:, 0].long(), x.argmax(dim=1))
     assert ctx.token_stats(x[:0], top=2)["top_ids"].shape == (0, 2)
+
+
+def test_another_stream():
+    import torch
+    from paper_2509_19086_b200 import binding
+    x = torch.randn(300, 1000, device="cuda")
+    side = torch.cuda.Stream()
+    with binding.Sja(stream=side.cuda_stream) as other:
+        side.wait_stream(torch.cuda.current_stream())
+        _check(other, x, np.arange(300), 5, wait=side.synchronize)
 
 
 def test_row_offsets_beyond_32_bits(ctx):
