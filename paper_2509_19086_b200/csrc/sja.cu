@@ -360,7 +360,7 @@ cudaError_t sorted_smem_attr() {
 template <typename T, int LOG>
 cudaError_t ssm_smem_attr() {
     const cudaError_t e = cudaFuncSetAttribute(ssm_step_many_kernel<T, LOG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               ssm_step_stages<LOG>() * (int)SSM_STEP_THREADS * (4 << LOG) * (int)sizeof(float));
+                                               (int)(SSM_STEP_STAGES * SSM_STEP_THREADS * (4u << LOG) * sizeof(float)));
     if constexpr (LOG > 0) return e == cudaSuccess ? ssm_smem_attr<T, LOG - 1>() : e;
     return e;
 }
@@ -613,8 +613,8 @@ sja_status sja_create(sja_ctx** out, int device, void* cuda_stream) {
             st = SJA_ERR_CUDA;
             break;
         }
-        if (ssm_smem_attr<float, 4>() != cudaSuccess || ssm_smem_attr<__half, 4>() != cudaSuccess ||
-            ssm_smem_attr<__nv_bfloat16, 4>() != cudaSuccess) { st = SJA_ERR_CUDA; break; }
+        if (ssm_smem_attr<float, 3>() != cudaSuccess || ssm_smem_attr<__half, 3>() != cudaSuccess ||
+            ssm_smem_attr<__nv_bfloat16, 3>() != cudaSuccess) { st = SJA_ERR_CUDA; break; }
         if ((st = reserve(c, c->gap_info, sizeof(GapInfo))) != SJA_OK) break;
     } while (0);
     if (st != SJA_OK) {
@@ -1536,26 +1536,24 @@ sja_status ssm_args(sja_ctx* c, const sja_ssm* m, uint32_t S, uint64_t n_rows, c
     return SJA_OK;
 }
 
-// Warps an SM that a prompt aims at by splitting the token axis (16 of 128 registers fit).
-#ifndef SSM_WARPS_PER_SM
-#define SSM_WARPS_PER_SM 16u
-#endif
-#ifndef SSM_FEW
-#define SSM_FEW 65536u
-#endif
-#ifndef SSM_BY_JOB
-#define SSM_BY_JOB 256u
-#endif
+// How a prompt is cut (times of a B200, inputs cold):
+// Warps an SM that it aims at by splitting the token axis; 16 of 128 registers fit.  65 536 tokens of one job, 1024
+// channels: 12 warps 1150 us, 16 warps 867 us, 24 warps 937 us.
+constexpr uint32_t SSM_WARPS_PER_SM = 16;
+// Up to so many values (tokens times channels) four lanes share a channel: that is bound by the time a warp takes for a
+// token.  500 tokens x 512: 46 us with one lane, 29 with four; 4500 x 512: 105 and 66; 4600 x 1024 (8 states): 80 and 136.
+constexpr uint64_t SSM_FEW = 1u << 22;
+// Up to so many tokens the jobs are walked whole, a CTA each, and nothing is handed on.  Jobs of 16 .. 48 tokens: 18 us
+// (39 in segments); two passes over 500 tokens of one job take 46 us, one pass over all of them 184.
+constexpr uint64_t SSM_BY_JOB = 256;
 template <typename T>
 sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
     if (a.T > 0) {
-        // A short prompt of few channels is bound by the time one warp takes for a token: four lanes share a channel.
-        const bool few = a.T * a.D <= SSM_FEW;
-        const SsmShape sh = ssm_shape(a.N, few);
+        const SsmShape sh = ssm_shape(a.N, a.T * a.D <= SSM_FEW);
         const uint32_t Dg = a.D / a.G, unit = 32u / sh.lanes;          // channels of a warp
         const uint32_t need = (Dg + unit - 1u) / unit;                 // warps of one group's channels
         // the widest CTA that leaves the fewest warps without a channel (they share the tile of B and C)
-        uint32_t warps = few ? 4u : SSM_THREADS / 32u;
+        uint32_t warps = sh.lanes == 4u ? 4u : SSM_THREADS / 32u;      // (f32, 64 states: 8 warps 369 us, 4 warps 349 us)
         while (warps > 1u && (need + warps - 1u) / warps * warps > (need + warps / 2u - 1u) / (warps / 2u) * (warps / 2u)) warps /= 2u;
         const uint32_t tiles = (need + warps - 1u) / warps * a.G;
         const uint64_t all = (uint64_t)need * a.G;
@@ -1563,8 +1561,8 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
         n_seg = std::min<uint64_t>(n_seg, (a.T + 31u) / 32u);
         if (n_seg < 3u && a.S == 1u) n_seg = 1u;                       // (two passes over half the tokens gain nothing)
         // about as many segments as jobs: then one each, which jobs of one length need not be cut for
-        if (a.S > 1u && 3ull * a.S >= 2u * n_seg && a.S <= 2u * n_seg) n_seg = a.S;
-        // a short prompt is not cut: a CTA per job, and nothing to hand on
+        // (150 jobs of 16 .. 4096 tokens: 98 segments 1445 us, 150 segments 1251 us)
+        if (a.S > 1u && 3ull * a.S >= n_seg * 2u && a.S <= 2u * n_seg) n_seg = a.S;
         a.by_job = a.T <= SSM_BY_JOB && a.S <= 65535u ? 1u : 0u;
         if (a.by_job) n_seg = a.S;
         n_seg = std::min<uint64_t>(n_seg, 65535u);
@@ -1590,18 +1588,14 @@ sja_status run_ssm_prompt(sja_ctx* c, SsmArgs& a) {
     return SJA_OK;
 }
 
-#ifndef SSM_STEP_MANY
-#define SSM_STEP_MANY 4u
-#endif
 template <typename T, int LOG>
 sja_status launch_ssm_step_many(sja_ctx* c, const SsmArgs& a) {
     const uint32_t np = 4u << LOG, tiles = (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS;
     const uint64_t values = (uint64_t)a.S * 2u * a.G * np;
     TRY(reserve(c, c->ssm_ws, values * sizeof(float)));
     launch_dep(ssm_step_bc_kernel<T>, dim3((uint32_t)((values + 255u) / 256u)), 256, 0, c->stream, a, np, c->ssm_ws.as<float>());
-    const uint32_t smem = (uint32_t)ssm_step_stages<LOG>() * SSM_STEP_THREADS * a.N * sizeof(float);
-    const uint32_t ctas = LOG <= 3 ? 2u : 1u;              // that fit an SM (registers, 96 or 128 KB of shared memory)
-    const uint32_t rows = std::max<uint32_t>(1u, (uint32_t)c->n_sm * ctas / tiles);
+    const uint32_t smem = SSM_STEP_STAGES * SSM_STEP_THREADS * a.N * sizeof(float);
+    const uint32_t rows = std::max<uint32_t>(1u, (uint32_t)c->n_sm * 2u / tiles);      // two CTAs fit an SM
     launch_dep(ssm_step_many_kernel<T, LOG>, dim3(tiles, std::min<uint32_t>(rows, a.S)), SSM_STEP_THREADS, smem, c->stream, a,
                static_cast<const float*>(c->ssm_ws.p));
     CU(cudaGetLastError());
@@ -1613,12 +1607,15 @@ sja_status run_ssm_step(sja_ctx* c, const SsmArgs& a) {
     uint32_t log_lanes = 0u;
     while ((4u << log_lanes) < a.N) ++log_lanes;
     const uint32_t vec = a.N % 4u == 0u && aligned16(a.A) && aligned16(a.state) ? 1u : 0u;
-    // many jobs: persistent CTAs with the states streaming through shared memory
-    if (vec && a.N <= 64u && (a.G << (log_lanes + 3u)) <= SSM_STEP_THREADS && a.D <= 65535u * SSM_STEP_THREADS &&
-        (uint64_t)a.S * ((a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS) >= (uint64_t)SSM_STEP_MANY * c->n_sm)
-        return log_lanes == 0u ? launch_ssm_step_many<T, 0>(c, a) : log_lanes == 1u ? launch_ssm_step_many<T, 1>(c, a)
-               : log_lanes == 2u ? launch_ssm_step_many<T, 2>(c, a) : log_lanes == 3u ? launch_ssm_step_many<T, 3>(c, a)
-                                                                                       : launch_ssm_step_many<T, 4>(c, a);
+    // From a CTA's work per SM on: persistent CTAs with the states streaming through shared memory (1024 channels of 16
+    // states, 37 jobs 11 us against 12, 296 jobs 17 against 24; 64 states: 1200 jobs of 512 channels 121 us against 79,
+    // two stages of 64 KB being all that fits).
+    if (vec && a.N <= 32u && (a.G << (log_lanes + 3u)) <= SSM_STEP_THREADS &&
+        (uint64_t)a.S * ((a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS) >= (uint64_t)c->n_sm)
+        return log_lanes == 0u   ? launch_ssm_step_many<T, 0>(c, a)
+               : log_lanes == 1u ? launch_ssm_step_many<T, 1>(c, a)
+               : log_lanes == 2u ? launch_ssm_step_many<T, 2>(c, a)
+                                 : launch_ssm_step_many<T, 3>(c, a);
     const size_t smem = ((size_t)8u << log_lanes) * a.G * sizeof(float);
     // a job's channels are spread over up to eight CTAs (a portable cluster)
     const uint32_t ctas = std::min<uint32_t>(8u, (a.D + SSM_STEP_THREADS - 1u) / SSM_STEP_THREADS);

@@ -742,10 +742,10 @@ template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.
 // Then the states: a CTA keeps to 256 channels and goes from job to job, with the states of the next STAGES - 1 jobs on
 // their way into shared memory and the rows of the next one in registers, so that the memory never waits for a job's
 // arithmetic.  2^LOG lanes share a channel, four states each; up to 16 states A stays in registers.
-template <int LOG> __host__ __device__ constexpr int ssm_step_stages() { return LOG <= 3 ? 3 : 2; }
+constexpr uint32_t SSM_STEP_STAGES = 3;
 template <typename T, int LOG>
 __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(const SsmArgs a, const float* __restrict__ bc) {
-    constexpr uint32_t STAGES = ssm_step_stages<LOG>(), LANES = 1u << LOG, PASSES = LANES, PER = SSM_STEP_THREADS >> LOG;
+    constexpr uint32_t STAGES = SSM_STEP_STAGES, LANES = 1u << LOG, PASSES = LANES, PER = SSM_STEP_THREADS >> LOG;
     constexpr bool KEEP_A = LOG <= 2;
     extern __shared__ __align__(16) float s_state[];        // [STAGES][256 channels][N]
     __shared__ __align__(16) float s_bc[SSM_STEP_THREADS];  // B of group 0 .. G - 1, then C, each padded to 4 * LANES
