@@ -61,16 +61,18 @@ __device__ __forceinline__ float rcp_fast(float v) {
     return r;
 }
 
-constexpr float LN2 = 0.693147182f, LOG2E = 1.44269504f;
+constexpr float LN2 = 0.693147182f, LOG2E = 1.44269502f, LOG2E_REST = 1.92596303e-8f;   // log2(e) in two parts
 
 __device__ __forceinline__ float silu(float v) { return v * rcp_fast(1.0f + exp2_fast(-LOG2E * v)); }
 
 // softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|) in 0 .. 1.  Time steps of 0.001 and less come from very negative v,
 // where log(1 + e) would lose what 1 + e rounds away; log1p(e) / e is smooth on 0 .. 1 and fitted by a polynomial there
 // (Chebyshev interpolation, relative error 6e-8), which keeps the relative accuracy and spares the exponential unit,
-// which the scan is bound by.
+// which the scan is bound by.  What rounding -|v| log2(e) takes off its exponent (4e-7 of e where |v| is 7) is put back.
 __device__ __forceinline__ float softplus(float v) {
-    const float e = exp2_fast(-LOG2E * fabsf(v));
+    float m;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(v)), "f"(200.0f));          // 2^-288 is 0; infinity has no remainder
+    const float t = -LOG2E * m, r = fmaf(-LOG2E_REST, m, fmaf(-LOG2E, m, -t)), f = exp2_fast(t), e = fmaf(f, LN2 * r, f);
     float p = fmaf(e, 0.00525345793f, -0.0295885075f);
     p = fmaf(e, p, 0.0783616677f);
     p = fmaf(e, p, -0.136747703f);
