@@ -1659,9 +1659,7 @@ sja_status launch_token_stats(sja_ctx* c, const TokenArgs& a, uint32_t ctas) {
     return SJA_OK;
 }
 
-#ifndef TOK_MANY_ROWS
-#define TOK_MANY_ROWS 1000u
-#endif
+constexpr uint32_t TOK_MANY_ROWS = 1000;      // see token_stats_kernel
 template <typename T>
 sja_status run_token_stats(sja_ctx* c, const TokenArgs& a) {
     constexpr uint32_t n = RowView<T>::n;

@@ -221,6 +221,14 @@ __host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np 
 // convolved once per CTA into shared memory, one tile ahead of the walk; x, dt and z are P groups of four ahead.
 // CARRY = true is the first pass of a split: what the job that crosses the segment's end adds to its state inside the
 // segment, and its sum of time steps (exp(A sum dt) is the decay over the segment).
+//
+// Bound by the exponential unit (16 results a clock and SM): N + 5 of its operations a channel and token against 8 bytes,
+// and what the split computes twice.  A token of 32 channels is 155 warp instructions, 21 of them there (168 of its
+// cycles).  64 jobs x 1024 tokens x 2048 channels of 16 states, bf16: 1.06 ms, 59 % of the unit's rate at 1.9 GHz (the
+// GPU ran at 1.6); 65 536 tokens of one job x 1024, both passes: 0.86 ms.  Also built and measured: a channel on two lanes
+// (1.15 ms, shuffles), two channels a thread with packed arithmetic throughout (118 instructions, but 168 registers and
+// too few warps: 1.15 to 1.8 ms), the token's scalars in a phase of their own through shared memory (2.4 ms),
+// the next group's scalars between the states' chains (1.14 ms, spills).
 template <typename T, int K, int LPC, bool CARRY>
 __global__ void __launch_bounds__(SSM_THREADS, LPC > 1 && K <= 8 ? 3 : 2) ssm_prompt_kernel(const SsmArgs a) {
     constexpr uint32_t NP = K * LPC, TT = ssm_tile_tokens(NP), CPW = 32 / LPC, COLS = CARRY ? NP : 2 * NP;
@@ -493,7 +501,8 @@ __global__ void __launch_bounds__(SSM_THREADS, LPC > 1 && K <= 8 ? 3 : 2) ssm_pr
     }
 }
 
-// Second pass of a split: the state at each segment's end, in order along the token axis, one thread per state.
+// Second pass of a split: the state at each segment's end, in order along the token axis, one thread per state.  Bound by
+// latency, hence eight segments' values at a time (74 segments x 16 384 states: the whole prompt 912 -> 892 us).
 __global__ void __launch_bounds__(256) ssm_carry_kernel(const SsmArgs a) {
     dep_wait();
     const uint64_t DN = (uint64_t)a.D * a.N, i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -555,7 +564,9 @@ constexpr uint32_t SSM_STEP_THREADS = 256;
 // a thread), each thread works out convolution, time step and gate of one channel; then the states are advanced,
 // written back, and summed against C over the 2^log_lanes lanes of a channel.  The CTAs of a job form a cluster: each
 // convolves the job's B and C for itself, so the kept rows of B and C are replaced only when the whole cluster has
-// read them.  VEC: N is a multiple of four and the states are aligned.
+// read them.  VEC: N is a multiple of four and the states are aligned.  For few jobs, where it is bound by the latency of
+// two dependent loads and the launch (one job x 1024 channels x 16 states: 4 us above an empty launch); from a CTA's work
+// per SM on ssm_step_many_kernel is faster (512 jobs: 35 us against 22).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(SSM_STEP_THREADS, 4) ssm_step_kernel(const SsmArgs a, uint32_t log_lanes) {
     extern __shared__ __align__(16) float s_bc[];           // B of all groups, then C, each padded to 4 * lanes
@@ -744,7 +755,9 @@ template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.
 
 // Then the states: a CTA keeps to 256 channels and goes from job to job, with the states of the next STAGES - 1 jobs on
 // their way into shared memory and the rows of the next one in registers, so that the memory never waits for a job's
-// arithmetic.  2^LOG lanes share a channel, four states each; up to 16 states A stays in registers.
+// arithmetic.  2^LOG lanes share a channel, four states each; up to 16 states A stays in registers.  Bound by memory: each
+// state is read and written once (8 N bytes a channel).  4096 jobs x 2048 channels x 16 states: 226 us, 5.5 TB/s, 84 % of
+// the measured copy; a CTA per job took 417 us, and 292 us went to waiting for slot numbers read where they are needed.
 constexpr uint32_t SSM_STEP_STAGES = 3;
 template <typename T, int LOG>
 __global__ void __launch_bounds__(SSM_STEP_THREADS, 2) ssm_step_many_kernel(const SsmArgs a, const float* __restrict__ bc) {
