@@ -387,7 +387,8 @@ typedef enum { SJA_F32 = 0, SJA_F16 = 1, SJA_BF16 = 2 } sja_dtype;
  *     y_t[d]    = (sum_n C_t[g, n] h_t[d, n] + skip[d] x_t[d]) silu(z_t[d])
  *
  * All sums and states are 32-bit; y is rounded once.  W = 0 leaves row_t as it is (no convolution, no silu).
- * Rows may lie apart (strides in elements, a row itself is contiguous); no alignment beyond the element's own.
+ * Rows may lie apart (strides in elements, below 2^28; a row itself is contiguous); no alignment beyond the element's
+ * own.
  * y must not overlap an input.  Infinities and NaN travel as the formulas carry them, within their own job only.
  *
  * Between calls a job lives in a slot of two pools: its states, and the W - 1 rows before its next token (oldest

@@ -1469,9 +1469,6 @@ namespace {
 
 bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) == 0; }
 
-#ifndef SSM_K32
-#define SSM_K32 16u
-#endif
 // Instance of the prompt kernel for N states: K of them in each of the lanes that share a channel.  One lane exchanges
 // nothing; four let a prompt of few tokens and channels through sooner, and hold wider states.
 struct SsmShape { uint32_t K, lanes; };
