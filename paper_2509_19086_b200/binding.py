@@ -418,7 +418,7 @@ class Sja:
         torch = _torch()
         code = self._rows("logits", logits, None, None)
         R, V = logits.size(0), logits.size(1)
-        if tokens is not None and not (tokens.dtype is torch.int64 and tokens.is_cuda and tokens.get_device() == self.device and
+        if tokens is not None and not (tokens.dtype is torch.int64 and tokens.get_device() == self.device and
                                        tokens.dim() == 1 and tokens.size(0) == R and tokens.is_contiguous()):
             self._flat("tokens", tokens, torch.int64, (R,))
         a = SjaTokenRows(code, top, R, V, scale, logits.data_ptr(), logits.stride(0) if R > 1 else V)
@@ -523,7 +523,7 @@ class SsmLayer:
 
     def _fill(self, xbc, dt, z, state, history, slots, n_jobs, out, more=()):
         """Check one call's tensors and write them into the call's arguments; returns (arguments, y).  The checks are
-        spelled out: a call for a few tokens lasts about as long as they do."""
+        spelled out (a tensor elsewhere has another device number): a call for a few tokens lasts about as long as they do."""
         ctx, torch, D, dev = self.ctx, _torch(), self.D, self.ctx.device
         a = SjaSsm.from_buffer_copy(self._args)
         a.dtype = ctx._rows("xbc", xbc, None, None)
@@ -531,21 +531,25 @@ class SsmLayer:
         if xbc.size(1) != self.rows:
             raise ValueError(f"xbc: rows of {xbc.size(1)}, not D + 2GN = {self.rows}")
         shape = (T, D)
-        ctx._rows("dt", dt, shape, row_type)
+        if not (dt.dtype is row_type and dt.get_device() == dev and dt.dim() == 2 and dt.size(0) == T and dt.size(1) == D and
+                dt.stride(1) == 1):
+            ctx._rows("dt", dt, shape, row_type)
         a.xbc, a.dt = xbc.data_ptr(), dt.data_ptr()
         if z is not None:
-            ctx._rows("z", z, shape, row_type)
+            if not (z.dtype is row_type and z.get_device() == dev and z.dim() == 2 and z.size(0) == T and z.size(1) == D and
+                    z.stride(1) == 1):
+                ctx._rows("z", z, shape, row_type)
             a.z = z.data_ptr()
         n_slots = n_jobs
         if state is not None:
-            if not (state.dtype is torch.float32 and state.is_cuda and state.get_device() == dev and state.dim() == 3 and
+            if not (state.dtype is torch.float32 and state.get_device() == dev and state.dim() == 3 and
                     state.size(1) == D and state.size(2) == self.N and state.is_contiguous()):
                 ctx._flat("state", state, torch.float32, (None, D, self.N))
             n_slots = state.size(0)
             a.state = state.data_ptr()
         if history is not None:
             keep = self.W - 1 if self.W > 1 else 0
-            if not (history.dtype is row_type and history.is_cuda and history.get_device() == dev and history.dim() == 3 and
+            if not (history.dtype is row_type and history.get_device() == dev and history.dim() == 3 and
                     history.size(1) == keep and history.size(2) == self.rows and history.is_contiguous() and
                     (state is None or history.size(0) == n_slots)):
                 ctx._flat("history", history, row_type, (None if state is None else n_slots, keep, self.rows))
@@ -554,7 +558,7 @@ class SsmLayer:
                 a.history = history.data_ptr()
         a.n_slots = n_slots
         if slots is not None:
-            if not (slots.dtype is torch.int32 and slots.is_cuda and slots.get_device() == dev and slots.dim() == 1 and
+            if not (slots.dtype is torch.int32 and slots.get_device() == dev and slots.dim() == 1 and
                     slots.size(0) == n_jobs and slots.is_contiguous()):
                 ctx._flat("slots", slots, torch.int32, (n_jobs,))
             a.slots = slots.data_ptr()
@@ -579,7 +583,7 @@ class SsmLayer:
         """sja_ssm_prompt: the packed tokens of S jobs, job s at rows ``off[s]`` .. ``off[s + 1] - 1`` (``off`` int64
         (S + 1,) on the device).  ``resume``: go on from the slots instead of from zero.  Returns y (T, D)."""
         ctx = self.ctx
-        if not (getattr(off, "dtype", None) is _torch().int64 and off.is_cuda and off.get_device() == ctx.device and off.dim() == 1 and
+        if not (getattr(off, "dtype", None) is _torch().int64 and off.get_device() == ctx.device and off.dim() == 1 and
                 off.is_contiguous()):
             ctx._flat("off", off, _torch().int64, (None,))
         S = off.size(0) - 1
