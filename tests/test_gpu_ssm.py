@@ -110,6 +110,30 @@ def test_prompt(ctx, shape, dtype):
         assert (c.state[rest] == before[0][rest]).all() and (c.history[rest] == before[1][rest]).all()
 
 
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("shape", [([700, 0, 300, 90], 67, 16, 4), ([400, 1, 2, 700], 64, 5, 3), ([1100], 66, 12, 4), ([250] * 5, 70, 9, 0),
+                                   ([1090], 65, 8, 1)], ids=str)
+def test_prompt_of_many_channels(ctx, shape, dtype):
+    """More than 2^22 values take the form with a channel per thread: the same channels 64 times over, each copy against
+    the reference of one."""
+    import torch
+    lens, D, N, W = shape
+    R = 64
+    for resume in (False, True):
+        c = Case(lens, D, N, 1, W, dtype, gate=not resume, seed=N, n_slots=len(lens) + 1)
+        want = c.want(resume)
+        over = lambda t, dim: torch.cat([t.narrow(dim, 0, D).repeat([R if i == dim else 1 for i in range(t.dim())]),
+                                         t.narrow(dim, D, t.shape[dim] - D)], dim)
+        cols = lambda t: None if t is None else t.repeat(1, R)
+        layer = ctx.ssm_layer(c.A.repeat(R, 1), conv_w=None if c.conv_w is None else over(c.conv_w, 0),
+                              conv_b=None if c.conv_b is None else over(c.conv_b, 0), skip=c.skip.repeat(R), dt_bias=c.dt_bias.repeat(R))
+        state, history = c.state.repeat(1, R, 1), over(c.history, 2).contiguous()
+        y = layer.prompt(over(c.xbc, 1), cols(c.dt), c.off, state=state, history=history, z=cols(c.z), slots=c.slots, resume=resume)
+        for copies in (y.view(-1, R, D), state.transpose(1, 2).reshape(-1, R, D), history[:, :, :R * D].reshape(-1, R, D)):
+            assert torch.equal(copies, copies[:, :1].expand_as(copies))
+        c.check(y[:, :D], state[:, :D], torch.cat([history[:, :, :D], history[:, :, R * D:]], 2), want)
+
+
 def test_prompt_is_deterministic_and_one_job_does_not_depend_on_the_others(ctx):
     import torch
     c = Case([400, 900, 77], 64, 16, seed=3, dtype="float32")
