@@ -207,7 +207,7 @@ template <int K> __device__ __forceinline__ void load_pairs(F2 (&to)[K / 2], con
 
 constexpr uint32_t SSM_THREADS = 256;    // most threads of a prompt CTA
 // Tokens whose B and C one CTA keeps at a time: a thread convolves a stretch of 8 tokens of one column (2 NP of them).
-__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np <= 64u ? 1024u / np : 16u; }
+__host__ __device__ constexpr uint32_t ssm_tile_tokens(uint32_t np) { return np <= 64u ? 1024u / np / 16u * 16u : 16u; }
 
 // Prompts.  LPC lanes share a channel, K of its states each, and walk a segment of the token axis with the states in
 // registers, four tokens at a time: each lane works out convolution, time step and gate of its own share of the four
